@@ -12,6 +12,9 @@
  * thc_quantize_rotated, thc_error_feedback / thc_accumulate_error (Algorithm 3's residual),
  * thc_aggregate_decompress (the last two in one launch, for a caller that holds every
  * worker's indices on one GPU).
+ * A program's gradients and weights are many tensors: thc_tensors_create makes a list of them,
+ * thc_grad_norm, thc_clip_grads and thc_gather_grads lead from it into a round, thc_scatter_grads
+ * and thc_adamw from a round's output back to it.
  *
  * Conventions shared by every call
  *   - "device" pointers are CUDA device addresses on the device that was current when the
@@ -60,6 +63,7 @@ extern "C" {
 
 #define THC_F32   0u
 #define THC_BF16  1u
+#define THC_F16   2u             /* tensors of a list only */
 
 #define THC_MAX_WORKERS 64u
 
@@ -267,6 +271,106 @@ int thc_error_feedback(thc_ctx *ctx, const void *const *grads, const void *const
 /* Algorithm 3, "x_i = grad_i + e_i": grads[i] += ef[i] in place, fp32, d elements each. */
 int thc_accumulate_error(thc_ctx *ctx, float *const *grads, const float *const *ef,
                          uint32_t n_local, uint64_t d, void *stream);
+
+/* ---- lists of tensors
+ *
+ * A list names, for each of n workers, `count` tensors: the same sizes and types for every worker, at
+ * addresses of their own.  In a flat vector (what thc_compress reads and thc_decompress writes) tensor t
+ * of a list starts at offsets[t], a multiple of THC_TENSOR_ALIGN elements; the up to THC_TENSOR_ALIGN - 1
+ * elements between one tensor's end and the next one's start belong to no tensor.  The calls below
+ * take tensors at any address that suits their type.  A list is a plan that a program keeps: it holds
+ * addresses, not the tensors, which stay the caller's. */
+#define THC_TENSOR_ALIGN 64u
+
+typedef struct thc_tensors thc_tensors;   /* opaque */
+
+typedef struct thc_tensors_sizes_t {
+    uint64_t d;                /* length of the flat vector, a multiple of THC_TENSOR_ALIGN    */
+    uint64_t elements;         /* elements of one worker's tensors                             */
+    uint64_t workspace_bytes;  /* scratch any of the calls may need for this list              */
+    uint32_t n;
+    uint32_t count;
+    int32_t device;            /* the context's, -1 without one                                */
+} thc_tensors_sizes_t;
+
+/* Make a list.  With a device, allocates device memory for its tables (16 bytes per 2048 elements and 8
+ * per tensor and worker) and synchronises: make lists before a stream capture.  In a context without
+ * device the list answers thc_tensors_sizes and thc_tensors_offsets.
+ *   tensors  host array of n * count device pointers, worker after worker; NULL is allowed where numel
+ *            is 0.  Each is aligned to its element size; contiguous.
+ *   numel    host array of `count` sizes, at least one above 0, 2^40 in all at most
+ *   dtype    host array of `count` THC_F32 / THC_BF16 / THC_F16
+ *   n        1..THC_MAX_WORKERS;  count  1..2^20
+ * thc_tensors_destroy synchronises the device (cudaFree). */
+int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uint64_t *numel, const uint32_t *dtype,
+                       uint32_t n, uint32_t count, thc_tensors **list);
+int thc_tensors_destroy(thc_tensors *list);
+int thc_tensors_sizes(const thc_tensors *list, thc_tensors_sizes_t *sizes);
+/* offsets: host array of `count` entries, written. */
+int thc_tensors_offsets(const thc_tensors *list, uint64_t *offsets);
+
+/* New addresses for the same sizes and types (gradients that are allocated anew every step), from the calls
+ * on that are issued on `stream` afterwards.  Allocates nothing; may be captured (a replay sets the addresses
+ * that were given at capture, which the checks of later calls do not know of). */
+int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *list, const void *const *tensors, void *stream);
+
+/* Global L2 norm of each worker's tensors: norms[i] = sqrt(sum over all tensors of worker i of x^2), squares
+ * summed in fp64 in a fixed order (the same bits on every call).  A tensor that stands in the list twice
+ * counts twice.  A norm that is NaN or infinite sets THC_STATUS_NONFINITE.
+ *   norms  device, n fp32, written (4-byte aligned, here and below)                              */
+int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes,
+                  void *stream);
+
+/* Clipping by the global norm, per worker: y = c x with c = min(1, max_norm / (norm + 1e-6)), c formed in fp64,
+ * the product in fp32 and rounded to the tensor's type.  A NaN norm makes every element NaN; an infinite one makes
+ * the finite elements 0 and the others NaN (as the formula does) and either sets THC_STATUS_NONFINITE.
+ *   max_norm     >= 0; infinity: c = 1, only the norm is of interest
+ *   out_or_null  list with the same n, sizes and types that is written; NULL: in place.  Written tensors must not
+ *                overlap each other, nor a tensor that is read unless it is the same one (THC_EINVAL)      */
+int thc_clip_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const thc_tensors *out_or_null, float *norms,
+                   void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* The way into a round: each worker's tensors, clipped as by thc_clip_grads, to its flat vector of
+ * the context's input type, zeros where no tensor is.  With residuals (fp32 contexts only, THC_EUNSUPPORTED
+ * otherwise) this is also Algorithm 3's "x_i = grad_i + e_i": x = fma(c, grad, e), between the tensors e alone.
+ *   flats        host array of n device pointers, sizes.d elements each, written; apart from each other and
+ *                from the tensors
+ *   ef_or_null   host array of n device pointers, sizes.d fp32 each; ef[i] may be flats[i]
+ *   norms        device, n fp32, written; NULL if max_norm is infinite: no norm is computed                  */
+int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *const *ef_or_null,
+                     void *const *flats, float *norms, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* The way out of a round: the flat average that thc_decompress wrote, clipped by the norm of what belongs to
+ * tensors (its noise between them does not count), to the tensors of a list with n = 1, each in its type.
+ *   flat   device, sizes.d fp32, read; a tensor of the list may be its own place in it
+ *   norms  device, one fp32, written; NULL if max_norm is infinite                                          */
+int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const thc_tensors *list, float *norms,
+                      void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* The Adam step with decoupled weight decay on the flat average (g = c x, clipped as above):
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,   t = step + 1,
+ *     w = w (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ * If the norm is not finite nothing is updated, step included, and THC_STATUS_NONFINITE is set.  Learning
+ * rate and step count are read on the device, so that a captured step can be replayed.
+ *   grad    device, sizes.d fp32, read
+ *   list    n = 1: the model's weights, written
+ *   lr      device, one fp32;   step  device, one int64 (steps done so far), t is written back
+ *   master  device, sizes.d fp32: w, from which the tensors are rounded; NULL: the tensors are w
+ *           themselves and all of them fp32 (THC_EINVAL otherwise)
+ *   m, v    device, sizes.d fp32 each
+ *   decay_or_null  device, `count` fp32: wd of each tensor (NULL: cfg.weight_decay for all)
+ *   norms   device, one fp32, written
+ * Nothing that is written may overlap anything else (THC_EINVAL); between the tensors master, m and v are
+ * neither read nor written. */
+typedef struct thc_adamw_config {
+    double beta1, beta2;       /* 0 <= beta < 1                             */
+    double eps;                /* >= 0                                      */
+    double weight_decay;       /* >= 0                                      */
+    double max_norm;           /* >= 0; infinity: no clipping               */
+} thc_adamw_config;
+int thc_adamw(thc_ctx *ctx, const thc_adamw_config *cfg, const float *grad, const thc_tensors *list, const float *lr,
+              int64_t *step, float *master_or_null, float *m, float *v, const float *decay_or_null, float *norms,
+              void *workspace, uint64_t workspace_bytes, void *stream);
 
 /* Read and clear the status bits (synchronises `stream`).  flags is a host pointer. */
 int thc_status(thc_ctx *ctx, uint32_t *flags, void *stream);

@@ -11,6 +11,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
+#include <string.h>
 
 #include "../../include/thc.h"
 
@@ -271,11 +272,160 @@ static PyObject *b_prepare_noalloc(ARGS)
     CALL(thc_prepare_noalloc((in_t)g.p, g.n, d, k, dtype, t_p, scales, status, st));
 }
 
+/* ---- lists of tensors.  What these calls take besides is as long as the list says; a torch tensor that is
+ * shorter, of another type, not contiguous or elsewhere is refused here, as the library sees only its address. */
+static PyObject *s_dtype, *s_is_contiguous, *s_get_device;
+static PyObject *tensor_type, *t_f32, *t_bf16, *t_i64;    /* of torch, looked up on first use */
+
+static int torch_names(void)
+{
+    if (t_i64 != NULL) return 0;
+    PyObject *m = PyImport_ImportModule("torch");
+    if (m == NULL) return -1;
+    if (tensor_type == NULL) tensor_type = PyObject_GetAttrString(m, "Tensor");
+    if (t_f32 == NULL) t_f32 = PyObject_GetAttrString(m, "float32");
+    if (t_bf16 == NULL) t_bf16 = PyObject_GetAttrString(m, "bfloat16");
+    if (tensor_type != NULL && t_f32 != NULL && t_bf16 != NULL) t_i64 = PyObject_GetAttrString(m, "int64");
+    Py_DECREF(m);
+    return t_i64 != NULL ? 0 : -1;
+}
+
+static int list_of(PyObject *o, thc_tensors **list, thc_tensors_sizes_t *sz)
+{
+    void *p;
+    memset(sz, 0, sizeof *sz);
+    if (address(o, &p) != 0 || torch_names() != 0) return -1;
+    *list = (thc_tensors *)p;
+    if (p != NULL) thc_tensors_sizes(*list, sz);
+    return 0;
+}
+
+enum { F32, BF16, I64 };
+static int vector(PyObject *o, void **p, int type, uint64_t elements, const thc_tensors_sizes_t *sz, const char *what)
+{
+    if (address(o, p) != 0) return -1;
+    if (o == Py_None || PyLong_Check(o) || sz->n == 0) return 0;
+    const int is = PyObject_IsInstance(o, tensor_type);
+    if (is <= 0) return is;
+    PyObject *t = PyObject_GetAttr(o, s_dtype);
+    if (t == NULL) return -1;
+    const int same = t == (type == F32 ? t_f32 : type == BF16 ? t_bf16 : t_i64);
+    Py_DECREF(t);
+    PyObject *c = PyObject_CallMethodNoArgs(o, s_is_contiguous), *v = PyObject_GetAttr(o, s_nbytes),
+             *g = PyObject_CallMethodNoArgs(o, s_get_device);
+    uint64_t bytes = 0;
+    int ok = c != NULL && v != NULL && g != NULL && number(v, &bytes) == 0;
+    const long device = ok ? PyLong_AsLong(g) : 0;
+    if (PyErr_Occurred()) ok = 0;
+    if (ok && !(same && c == Py_True && bytes >= elements * (type == F32 ? 4u : type == BF16 ? 2u : 8u) && device == sz->device)) {
+        PyErr_Format(PyExc_ValueError, "%s: a contiguous %s tensor of at least %llu elements on the context's device is expected", what,
+                     type == F32 ? "float32" : type == BF16 ? "bfloat16" : "int64", (unsigned long long)elements);
+        ok = 0;
+    }
+    Py_XDECREF(c);
+    Py_XDECREF(v);
+    Py_XDECREF(g);
+    return ok ? 0 : -1;
+}
+
+/* One vector per worker. */
+static int vectors(PyObject *o, list_t *out, int type, const thc_tensors_sizes_t *sz, const char *what)
+{
+    out->n = 0;
+    out->given = o != Py_None;
+    if (!out->given) return 0;
+    PyObject *seq = PySequence_Fast(o, "a sequence of tensors is expected");
+    if (seq == NULL) return -1;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    int rc = 0;
+    if (sz->n != 0 && n != (Py_ssize_t)sz->n) {
+        PyErr_Format(PyExc_ValueError, "%s: one per worker is expected", what);
+        rc = -1;
+    }
+    for (Py_ssize_t i = 0; rc == 0 && i < n && i < (Py_ssize_t)THC_MAX_WORKERS; ++i)
+        rc = vector(PySequence_Fast_GET_ITEM(seq, i), &out->p[i], type, sz->d, sz, what);
+    out->n = (uint32_t)n;
+    Py_DECREF(seq);
+    return rc;
+}
+
+static int real(PyObject *o, double *v)
+{
+    *v = PyFloat_AsDouble(o);
+    return *v == -1.0 && PyErr_Occurred() ? -1 : 0;
+}
+
+#define LIST_CALL thc_tensors *list; thc_tensors_sizes_t sz; uint64_t wb; void *ws
+
+/* (handle, list, norms, workspace, stream) */
+static PyObject *b_grad_norm(ARGS)
+{
+    BEGIN(5);
+    LIST_CALL;
+    void *norms;
+    if (list_of(a[1], &list, &sz) || vector(a[2], &norms, F32, sz.n, &sz, "norms") || workspace(a[3], &ws, &wb)) return NULL;
+    CALL(thc_grad_norm(ctx, list, norms, ws, wb, st));
+}
+
+/* (handle, list, max_norm, out, norms, workspace, stream) */
+static PyObject *b_clip_grads(ARGS)
+{
+    BEGIN(7);
+    LIST_CALL;
+    double most;
+    void *out, *norms;
+    if (list_of(a[1], &list, &sz) || real(a[2], &most) || address(a[3], &out) || vector(a[4], &norms, F32, sz.n, &sz, "norms") ||
+        workspace(a[5], &ws, &wb)) return NULL;
+    CALL(thc_clip_grads(ctx, list, most, out, norms, ws, wb, st));
+}
+
+/* (handle, list, max_norm, ef, flats, norms, workspace, bf16, stream) */
+static PyObject *b_gather_grads(ARGS)
+{
+    BEGIN(9);
+    LIST_CALL;
+    double most;
+    list_t e, f;
+    void *norms;
+    const int type = PyObject_IsTrue(a[7]) ? BF16 : F32;
+    if (list_of(a[1], &list, &sz) || real(a[2], &most) || vectors(a[3], &e, F32, &sz, "ef") || vectors(a[4], &f, type, &sz, "flats") ||
+        vector(a[5], &norms, F32, sz.n, &sz, "norms") || workspace(a[6], &ws, &wb)) return NULL;
+    CALL(thc_gather_grads(ctx, list, most, (const float *const *)array_of(&e), array_of(&f), norms, ws, wb, st));
+}
+
+/* (handle, flat, max_norm, list, norms, workspace, stream) */
+static PyObject *b_scatter_grads(ARGS)
+{
+    BEGIN(7);
+    LIST_CALL;
+    double most;
+    void *flat, *norms;
+    if (list_of(a[3], &list, &sz) || vector(a[1], &flat, F32, sz.d, &sz, "flat") || real(a[2], &most) ||
+        vector(a[4], &norms, F32, sz.n, &sz, "norms") || workspace(a[5], &ws, &wb)) return NULL;
+    CALL(thc_scatter_grads(ctx, flat, most, list, norms, ws, wb, st));
+}
+
+/* (handle, (beta1, beta2, eps, weight_decay, max_norm), grad, list, lr, step, master, m, v, decay, norms, workspace, stream) */
+static PyObject *b_adamw(ARGS)
+{
+    BEGIN(13);
+    LIST_CALL;
+    thc_adamw_config cfg;
+    void *grad, *lr, *step, *master, *m, *v, *decay, *norms;
+    if (!PyArg_ParseTuple(a[1], "ddddd", &cfg.beta1, &cfg.beta2, &cfg.eps, &cfg.weight_decay, &cfg.max_norm)) return NULL;
+    if (list_of(a[3], &list, &sz) || vector(a[2], &grad, F32, sz.d, &sz, "grad") || vector(a[4], &lr, F32, 1, &sz, "lr") ||
+        vector(a[5], &step, I64, 1, &sz, "step") || vector(a[6], &master, F32, sz.d, &sz, "master") ||
+        vector(a[7], &m, F32, sz.d, &sz, "m") || vector(a[8], &v, F32, sz.d, &sz, "v") ||
+        vector(a[9], &decay, F32, sz.count, &sz, "decay") || vector(a[10], &norms, F32, 1, &sz, "norms") || workspace(a[11], &ws, &wb)) return NULL;
+    CALL(thc_adamw(ctx, &cfg, grad, list, lr, step, master, m, v, decay, norms, ws, wb, st));
+}
+
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))b_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     ENTRY(prepare), ENTRY(prepare_minmax), ENTRY(compress), ENTRY(prepare_compress), ENTRY(quantize_rotated),
     ENTRY(aggregate), ENTRY(decompress), ENTRY(aggregate_decompress), ENTRY(error_feedback),
-    ENTRY(accumulate_error), ENTRY(prepare_noalloc), {NULL, NULL, 0, NULL}};
+    ENTRY(accumulate_error), ENTRY(prepare_noalloc), ENTRY(grad_norm), ENTRY(clip_grads), ENTRY(gather_grads),
+    ENTRY(scatter_grads), ENTRY(adamw), {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -284,6 +434,10 @@ PyMODINIT_FUNC PyInit__binding(void)
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (s_data_ptr == NULL || s_nbytes == NULL || s_cuda_stream == NULL) return NULL;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    if (s_data_ptr == NULL || s_nbytes == NULL || s_cuda_stream == NULL || s_dtype == NULL || s_is_contiguous == NULL ||
+        s_get_device == NULL) return NULL;
     return PyModule_Create(&module);
 }

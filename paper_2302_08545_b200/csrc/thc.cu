@@ -683,6 +683,7 @@ aggregate_kernel(PtrArray in, uint32_t n, uint64_t units, uint64_t d_pad, const 
 
 #include "thc_pipeline.cuh"
 #include "thc_block.h"
+#include "thc_host.h"
 
 // =========================================================================== host side
 using namespace thc;
@@ -714,36 +715,13 @@ struct thc_ctx {
 static thread_local cudaError_t g_last_cuda = cudaSuccess;
 static thread_local char g_err_text[256];
 
-static int cuda_fail(cudaError_t e)
+int thc::cuda_fail(cudaError_t e)
 {
     g_last_cuda = e;
     return THC_ECUDA;
 }
 
-#define THC_CUDA(...)                                         \
-    do {                                                      \
-        cudaError_t e__ = (__VA_ARGS__);                      \
-        if (e__ != cudaSuccess) return cuda_fail(e__);        \
-    } while (0)
-
-// A launch that may start while the one before it on the stream is still running (depend_on_previous):
-// 1 to 1.5 us less between two launches of a round.
-template <class... P, class... A>
-static cudaError_t launch_after(void (*kern)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A... args)
-{
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, P(args)...);
-}
+CtxView thc::view_of(const thc_ctx *ctx) { return CtxView{ctx->dev, ctx->device, ctx->sm_count, ctx->cfg.in_dtype}; }
 
 // No launch takes more dynamic shared memory: a pipeline CTA, a tile of 2^14 or one of 2^13 with the constants
 // of 1024 blocks, each with a table of 256 entries, take up to 101 KB.  (More than half an SM's 228 KB, so that
@@ -794,8 +772,6 @@ static cudaError_t count_lone_clusters(int sm_count, int *n)
     shape.numAttrs = 1;
     return cudaOccupancyMaxActiveClusters(n, kern, &shape);
 }
-
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 const char *thc_version(void) { return "thc-b200 0.1 (sm_100a)"; }
 
@@ -1057,7 +1033,7 @@ int thc_sizes(const thc_ctx *ctx, uint64_t d, uint32_t n_local, thc_sizes_t *s)
     return THC_OK;
 }
 
-static int check_launch_ctx(const thc_ctx *ctx)
+int thc::check_launch_ctx(const thc_ctx *ctx)
 {
     if (ctx == nullptr) return THC_EINVAL;
     if (ctx->device < 0 || ctx->dev == nullptr) { g_last_cuda = cudaSuccess; return THC_ECUDA; }

@@ -1,0 +1,904 @@
+// Lists of tensors around a round: global norm, clipping, the ways into and out of the flat vector, the Adam step.
+// See include/thc.h for the contract of every entry point.
+//
+// All of it is streaming: two to twenty operations per element against 2 to 30 bytes, so the loads are what the
+// kernels are built around.  A list is cut into pieces of at most 2048 elements of one tensor, and a warp takes a piece
+// at a time with all loads of half or all of it in flight.  The table of pieces is made once per list; a piece
+// names its flat position, from which every address follows (the table of tensor addresses holds the address that
+// flat position 0 would have).
+//
+// Clipping needs the norm of everything before the first product, so a call is two launches: the sums, whose last
+// CTA forms norm and factor, and the products, which go through the pieces backwards because what was
+// read last is still in L2.
+#include "thc_host.h"
+
+#include <algorithm>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <new>
+#include <type_traits>
+#include <vector>
+
+namespace thc {
+
+constexpr uint32_t kPiece = 2048;              // elements of a piece: eight units of eight per lane
+constexpr uint32_t kUnit = 8;                  // consecutive elements of a lane: 16 bytes of a 16-bit type, 32 of fp32
+constexpr int kListThreads = 256, kListWarps = kListThreads / 32;
+constexpr uint32_t kNormCtasPerSm = 4, kMoveCtasPerSm = 4;
+
+// {flat position (64 bits), tensor, length (16 bits) and type}
+struct Piece { uint64_t flat; uint32_t tensor, len_type; };
+static_assert(sizeof(Piece) == 16, "one load");
+
+struct ListTable {
+    const Piece *pieces;
+    const uint64_t *base;        // [n][count]: address of the tensor less its flat position, in bytes
+    uint32_t count, pieces_n;
+};
+
+// The factor c of the products as two: c x = factor (x scale).  Where c is an fp32 denormal (gradients near fp32's end)
+// scale is 2^-126 and factor keeps all its bits: x scale is exact wherever c x is not itself a denormal.  Else scale is 1.
+struct Factor { float factor, scale; };
+__device__ __forceinline__ float times(const Factor &c, float x) { return c.factor * (x * c.scale); }
+
+// What the sums' last CTA leaves for the products.
+struct alignas(16) NormResult { Factor c; uint32_t skip, pad_; float step_size, inv_sqrt_by2, pad2_[2]; };
+
+struct NormOut {
+    double *partial;             // [n][gridDim.x]
+    NormResult *result;          // [n]
+    float *norms;                // or null
+    DeviceBlock *dev;
+    double max_norm;
+    // Adam step
+    const float *lr;             // null: none
+    int64_t *step;
+    double beta1, beta2;
+};
+
+__device__ __forceinline__ Piece load_piece(const Piece *p)
+{
+    const uint4 q = __ldg(reinterpret_cast<const uint4 *>(p));
+    return Piece{(uint64_t)q.x | (uint64_t)q.y << 32, q.z, q.w};
+}
+__device__ __forceinline__ uint64_t load_base(const uint64_t *p)
+{
+    uint64_t v;
+    asm volatile("ld.global.u64 %0, [%1];" : "=l"(v) : "l"(p));
+    return v;
+}
+
+// ------------------------------------------------------------------------------ elements
+// A unit as it is loaded (4 or 8 registers), and its values.
+template <uint32_t T> struct Raw { uint32_t w[T == THC_F32 ? 8 : 4]; };
+template <uint32_t T> __host__ __device__ constexpr uint32_t size_of() { return T == THC_F32 ? 4u : 2u; }
+
+template <uint32_t T>
+__device__ __forceinline__ Raw<T> load_unit8(uint64_t a)
+{
+    Raw<T> r;
+    if constexpr (T == THC_F32)
+        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(a));
+    else
+        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(a));
+    return r;
+}
+
+template <uint32_t T>
+__device__ __forceinline__ float widen16(uint32_t v)
+{
+    return T == THC_BF16 ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((unsigned short)v));
+}
+template <uint32_t T>
+__device__ __forceinline__ float value(const Raw<T> &r, int e)
+{
+    if constexpr (T == THC_F32) return __uint_as_float(r.w[e]);
+    const uint32_t w = r.w[e >> 1];
+    if (T == THC_BF16) return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
+    return widen16<T>(e & 1 ? w >> 16 : w & 0xFFFFu);
+}
+template <uint32_t T>
+__device__ __forceinline__ float load_one(uint64_t a)
+{
+    if (T == THC_F32) return ld_global(reinterpret_cast<const float *>(a));
+    return widen16<T>(ld_global(reinterpret_cast<const uint16_t *>(a)));
+}
+// The only rounding of a result: to nearest, ties to even.
+template <uint32_t T>
+__device__ __forceinline__ uint32_t narrow16(float v)
+{
+    return T == THC_BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)) : (uint32_t)__half_as_ushort(__float2half_rn(v));
+}
+template <uint32_t T>
+__device__ __forceinline__ void store_one(uint64_t a, float v)
+{
+    if (T == THC_F32) *reinterpret_cast<float *>(a) = v;
+    else *reinterpret_cast<uint16_t *>(a) = (uint16_t)narrow16<T>(v);
+}
+template <uint32_t T>
+__device__ __forceinline__ void store_unit8(uint64_t a, const float (&v)[8])
+{
+    if (T == THC_F32) {
+        asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                     :: "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(a) : "memory");
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = narrow16<T>(v[2 * i]) | narrow16<T>(v[2 * i + 1]) << 16;
+        asm volatile("st.global.v4.b32 [%4], {%0, %1, %2, %3};" :: "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(a) : "memory");
+    }
+}
+
+// Elements before the first one on a unit boundary.
+template <uint32_t T>
+__device__ __forceinline__ uint32_t head_of(uint64_t a) { return (uint32_t)((0ull - a) / size_of<T>()) & (kUnit - 1u); }
+
+// ---------------------------------------------------------------------------------- norm
+template <uint32_t T>
+__device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uint32_t lane)
+{
+    constexpr int kBatch = T == THC_F32 ? 4 : 8;
+    double s[2] = {0.0, 0.0};
+    const uint32_t head = min(head_of<T>(a), len), units = (len - head) / kUnit, tail = head + units * kUnit;
+    // lanes 0..7 the elements before the units, lanes 8..15 those behind
+    const uint32_t single = lane < 8u ? lane : tail + lane - 8u;
+    float edge = 0.0f;
+    if (lane < 8u ? single < head : lane < 16u && single < len) edge = load_one<T>(a + (uint64_t)single * size_of<T>());
+    uint64_t at = a + head * size_of<T>();
+    // a whole batch, or what is left: lanes without a unit load the last one again and add nothing
+    const auto batch = [&](auto whole, uint32_t left) {
+        Raw<T> r[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            r[b] = load_unit8<T>(decltype(whole)::value ? at + 32u * b * kUnit * size_of<T>()
+                                                        : at + min(lane + 32u * b, left - 1u) * (kUnit * size_of<T>()));
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            if (!decltype(whole)::value && lane + 32u * b >= left) r[b] = Raw<T>{};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double v = (double)value<T>(r[b], e);
+                s[e & 1] = fma(v, v, s[e & 1]);
+            }
+        }
+        at += 32u * kBatch * kUnit * size_of<T>();
+    };
+    uint32_t u = 0;
+#pragma unroll 1
+    for (at += lane * (kUnit * size_of<T>()); u + 32u * kBatch <= units; u += 32u * kBatch) batch(std::true_type{}, 0u);
+    at -= lane * (kUnit * size_of<T>());
+    if (u < units) batch(std::false_type{}, units - u);
+    const double v = (double)edge;
+    return fma(v, v, s[0]) + s[1];
+}
+
+__device__ __forceinline__ double squares(const ListTable &L, const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane)
+{
+    const uint32_t len = p.len_type & 0xFFFFu, type = p.len_type >> 16;
+    if (flat != 0) return squares_of_piece<THC_F32>(flat + p.flat * 4u, len, lane);
+    const uint64_t b = load_base(base + p.tensor);
+    if (type == THC_F32) return squares_of_piece<THC_F32>(b + p.flat * 4u, len, lane);
+    if (type == THC_BF16) return squares_of_piece<THC_BF16>(b + p.flat * 2u, len, lane);
+    return squares_of_piece<THC_F16>(b + p.flat * 2u, len, lane);
+}
+
+// Norm, factor and what the Adam step needs, from a worker's sum of squares.
+__device__ __forceinline__ void finish_norm(const NormOut &o, uint32_t worker, double sum)
+{
+    const double norm = sqrt(sum);
+    NormResult r{};
+    r.c = Factor{1.0f, 1.0f};
+    if (!isinf(o.max_norm)) {
+        const double c = o.max_norm / (norm + 1e-6);
+        if (c < 0x1p-126) r.c = Factor{(float)(c * 0x1p126), 0x1p-126f};
+        else r.c.factor = c > 1.0 ? 1.0f : (float)c;   // NaN stays
+    }
+    const bool finite = isfinite(norm);
+    if (!finite) atomicOr(&o.dev->status, THC_STATUS_NONFINITE);
+    if (o.norms != nullptr) o.norms[worker] = (float)norm;
+    if (o.lr != nullptr) {
+        r.skip = finite ? 0u : 1u;
+        if (finite) {
+            const int64_t t = *o.step + 1;
+            *o.step = t;
+            r.step_size = (float)((double)*o.lr / (1.0 - pow(o.beta1, (double)t)));
+            r.inv_sqrt_by2 = (float)(1.0 / sqrt(1.0 - pow(o.beta2, (double)t)));
+        }
+    }
+    o.result[worker] = r;
+}
+
+// Sums of squares of all pieces; a warp's pieces are fixed by the grid and the sums are added in a fixed order.
+__global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
+list_norm_kernel(const __grid_constant__ ListTable L, const __grid_constant__ NormOut o, uint64_t flat)
+{
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
+    const uint32_t stride = gridDim.x * kListWarps;
+    uint32_t c = blockIdx.x * kListWarps + warp;
+    Piece p{};
+    if (c < L.pieces_n) p = load_piece(L.pieces + c);   // written before any launch
+    depend_on_previous();
+    const uint64_t *base = L.base + (uint64_t)worker * L.count;
+    double s = 0.0;
+#pragma unroll 1
+    while (c < L.pieces_n) {
+        const Piece now = p;
+        c += stride;
+        if (c < L.pieces_n) p = load_piece(L.pieces + c);
+        s += squares(L, now, base, flat, lane);
+    }
+    __shared__ double red[kListWarps];
+    __shared__ uint32_t last;
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, off);
+    if (lane == 0) red[warp] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = 0.0;
+        for (int w = 0; w < kListWarps; ++w) t += red[w];
+        __stcg(o.partial + (uint64_t)worker * gridDim.x + blockIdx.x, t);
+        __threadfence();
+        last = atomicInc(o.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double t = 0.0;
+    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) t += __ldcg(o.partial + (uint64_t)worker * gridDim.x + i);
+    for (int off = 16; off > 0; off >>= 1) t += __shfl_down_sync(0xFFFFFFFFu, t, off);
+    if (lane == 0) red[warp] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        t = 0.0;
+        for (int w = 0; w < kListWarps; ++w) t += red[w];
+        finish_norm(o, worker, t);
+    }
+}
+
+// ---------------------------------------------------------------------------------- products
+// y = c x (+ e) for a piece; zeros (or e) from its end up to dst_len.
+template <uint32_t S, uint32_t D, bool EF>
+__device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t ef, uint32_t len, uint32_t dst_len, const Factor &c, uint32_t lane)
+{
+    const auto product = [&c](float x, float e) { return EF ? fmaf(c.factor, x * c.scale, e) : times(c, x); };
+    const uint32_t h = min(head_of<S>(src), len);
+    if (head_of<S>(src) == head_of<D>(dst) && (!EF || head_of<S>(src) == head_of<THC_F32>(ef))) {
+        constexpr int kBatch = EF ? 2 : S == THC_F32 ? 4 : 8;
+        const uint32_t units = (len - h) / kUnit;
+        uint64_t s = src + h * size_of<S>(), d = dst + h * size_of<D>(), q = ef + h * 4u;
+        // a whole batch, or what is left: lanes without a unit load the last one again and store nothing
+        const auto batch = [&](auto whole, uint32_t left) {
+            constexpr bool kWhole = decltype(whole)::value;
+            Raw<S> x[kBatch];
+            Raw<THC_F32> r[EF ? kBatch : 1];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                const uint32_t v = (kWhole ? lane + 32u * b : min(lane + 32u * b, left - 1u)) * kUnit;
+                x[b] = load_unit8<S>(s + v * size_of<S>());
+                if constexpr (EF) r[b] = load_unit8<THC_F32>(q + v * 4u);
+            }
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                if (!kWhole && lane + 32u * b >= left) break;
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = product(value<S>(x[b], e), EF ? value<THC_F32>(r[EF ? b : 0], e) : 0.0f);
+                store_unit8<D>(d + (lane + 32u * b) * (kUnit * size_of<D>()), y);
+            }
+            s += 32u * kBatch * kUnit * size_of<S>();
+            d += 32u * kBatch * kUnit * size_of<D>();
+            q += 32u * kBatch * kUnit * 4u;
+        };
+        uint32_t u = 0;
+#pragma unroll 1
+        for (; u + 32u * kBatch <= units; u += 32u * kBatch) batch(std::true_type{}, 0u);
+        if (u < units) batch(std::false_type{}, units - u);
+        // lanes 0..7 the elements before the units, lanes 8..15 those behind
+        const uint32_t i = lane < 8u ? lane : h + units * kUnit + lane - 8u;
+        if (lane < 8u ? i < h : lane < 16u && i < len) {
+            const float e = EF ? load_one<THC_F32>(ef + i * 4u) : 0.0f;
+            store_one<D>(dst + i * size_of<D>(), product(load_one<S>(src + i * size_of<S>()), e));
+        }
+    } else {
+        constexpr int kBatch = EF ? 8 : 16;
+        uint64_t s = src, d = dst, q = ef;
+        const auto batch = [&](auto whole, uint32_t left) {
+            constexpr bool kWhole = decltype(whole)::value;
+            float x[kBatch], r[EF ? kBatch : 1];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                const uint32_t v = kWhole ? lane + 32u * b : min(lane + 32u * b, left - 1u);
+                x[b] = load_one<S>(s + v * size_of<S>());
+                if constexpr (EF) r[b] = load_one<THC_F32>(q + v * 4u);
+            }
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                if (!kWhole && lane + 32u * b >= left) break;
+                store_one<D>(d + (lane + 32u * b) * size_of<D>(), product(x[b], EF ? r[EF ? b : 0] : 0.0f));
+            }
+            s += 32u * kBatch * size_of<S>();
+            d += 32u * kBatch * size_of<D>();
+            q += 32u * kBatch * 4u;
+        };
+        uint32_t j = 0;
+#pragma unroll 1
+        for (; j + 32u * kBatch <= len; j += 32u * kBatch) batch(std::true_type{}, 0u);
+        if (j < len) batch(std::false_type{}, len - j);
+    }
+    for (uint32_t j = len + lane; j < dst_len; j += 32u)
+        store_one<D>(dst + j * size_of<D>(), EF ? load_one<THC_F32>(ef + j * 4u) : 0.0f);
+}
+
+enum MoveKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter };
+
+struct MoveParams {
+    ListTable src, dst;          // kClip; kGather*: src; kScatter: dst
+    const NormResult *result;    // null: factor 1
+    uint64_t src_flat;           // kScatter
+    uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS];   // kGather*
+};
+
+template <MoveKind K, uint32_t T>
+__device__ __forceinline__ void move_typed(const MoveParams &P, const Piece &p, uint32_t worker, const Factor &c, uint32_t lane)
+{
+    const uint32_t len = p.len_type & 0xFFFFu;
+    const uint64_t at = p.flat * size_of<T>();
+    if (K == kClip) {
+        const uint64_t i = (uint64_t)worker * P.src.count + p.tensor;
+        move_piece<T, T, false>(load_base(P.src.base + i) + at, load_base(P.dst.base + i) + at, 0, len, len, c, lane);
+    } else if (K == kScatter) {
+        move_piece<THC_F32, T, false>(P.src_flat + p.flat * 4u, load_base(P.dst.base + p.tensor) + at, 0, len, len, c, lane);
+    } else {
+        constexpr uint32_t D = K == kGatherBf16 ? THC_BF16 : THC_F32;
+        const uint64_t src = load_base(P.src.base + (uint64_t)worker * P.src.count + p.tensor) + at;
+        const uint32_t full = (len + THC_TENSOR_ALIGN - 1u) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
+        move_piece<T, D, K == kGatherResidual>(src, P.dst_flat[worker] + p.flat * size_of<D>(),
+                                               K == kGatherResidual ? P.ef[worker] + p.flat * 4u : 0, len, full, c, lane);
+    }
+}
+
+template <MoveKind K>
+__global__ void __launch_bounds__(kListThreads, kMoveCtasPerSm)
+list_move_kernel(const __grid_constant__ MoveParams P)
+{
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
+    const ListTable &L = K == kScatter ? P.dst : P.src;
+    const uint32_t stride = gridDim.x * kListWarps;
+    uint32_t c = blockIdx.x * kListWarps + warp;
+    Piece p{};
+    if (c < L.pieces_n) p = load_piece(L.pieces + (L.pieces_n - 1u - c));
+    depend_on_previous();
+    Factor factor{1.0f, 1.0f};
+    if (P.result != nullptr) {
+        const uint2 q = ld_global(reinterpret_cast<const uint2 *>(&P.result[worker].c));
+        factor = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
+    }
+#pragma unroll 1
+    while (c < L.pieces_n) {
+        const Piece now = p;
+        c += stride;
+        if (c < L.pieces_n) p = load_piece(L.pieces + (L.pieces_n - 1u - c));
+        const uint32_t type = now.len_type >> 16;
+        if (type == THC_F32) move_typed<K, THC_F32>(P, now, worker, factor, lane);
+        else if (type == THC_BF16) move_typed<K, THC_BF16>(P, now, worker, factor, lane);
+        else move_typed<K, THC_F16>(P, now, worker, factor, lane);
+    }
+}
+
+// ---------------------------------------------------------------------------------- Adam
+struct AdamParams {
+    ListTable L;
+    const NormResult *result;
+    const float *grad;
+    float *master, *m, *v;       // master null: the tensors are the weights
+    const float *lr, *decay;     // decay null: weight_decay
+    float beta1, beta2, one_less_beta1, one_less_beta2, eps;
+    double weight_decay;
+};
+
+struct AdamStep { Factor c; float b1, b2, a1, a2, eps, step_size, inv_sqrt_by2, keep; };
+
+// m and v in place; the new weight.
+__device__ __forceinline__ float adam(const AdamStep &k, float g, float &m, float &v, float w)
+{
+    g = times(k.c, g);
+    m = fmaf(k.b1, m, k.a1 * g);
+    v = fmaf(k.b2, v, k.a2 * g * g);
+    const float move = m / fmaf(sqrtf(v), k.inv_sqrt_by2, k.eps);
+    return fmaf(-k.step_size, move, w * k.keep);
+}
+
+template <uint32_t T, bool MASTER>
+__device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &k, const Piece &p, uint32_t lane)
+{
+    const uint32_t len = p.len_type & 0xFFFFu;
+    const uint64_t at = p.flat * 4u;
+    const uint64_t g = reinterpret_cast<uint64_t>(P.grad) + at, m = reinterpret_cast<uint64_t>(P.m) + at,
+                   v = reinterpret_cast<uint64_t>(P.v) + at, out = load_base(P.L.base + p.tensor) + p.flat * size_of<T>();
+    const uint64_t w = MASTER ? reinterpret_cast<uint64_t>(P.master) + at : out;
+    uint32_t done = 0;
+    if (((g | m | v | w) & 31u) == 0 && head_of<T>(out) == 0u) {
+        const uint32_t units = len / kUnit;
+        done = units * kUnit;
+#pragma unroll 1
+        for (uint32_t u = lane; u < units; u += 32u) {
+            const uint64_t o = (uint64_t)u * (kUnit * 4u);
+            const Raw<THC_F32> rg = load_unit8<THC_F32>(g + o), rm = load_unit8<THC_F32>(m + o), rv = load_unit8<THC_F32>(v + o),
+                               rw = load_unit8<THC_F32>(w + o);
+            float ym[8], yv[8], yw[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ym[e] = value<THC_F32>(rm, e);
+                yv[e] = value<THC_F32>(rv, e);
+                yw[e] = adam(k, value<THC_F32>(rg, e), ym[e], yv[e], value<THC_F32>(rw, e));
+            }
+            store_unit8<THC_F32>(m + o, ym);
+            store_unit8<THC_F32>(v + o, yv);
+            if (MASTER) store_unit8<THC_F32>(w + o, yw);
+            store_unit8<T>(out + (uint64_t)u * (kUnit * size_of<T>()), yw);
+        }
+    }
+    for (uint32_t j = done + lane; j < len; j += 32u) {
+        const uint64_t o = (uint64_t)j * 4u;
+        float ym = load_one<THC_F32>(m + o), yv = load_one<THC_F32>(v + o);
+        const float yw = adam(k, load_one<THC_F32>(g + o), ym, yv, load_one<THC_F32>(w + o));
+        store_one<THC_F32>(m + o, ym);
+        store_one<THC_F32>(v + o, yv);
+        if (MASTER) store_one<THC_F32>(w + o, yw);
+        store_one<T>(out + (uint64_t)j * size_of<T>(), yw);
+    }
+}
+
+template <bool MASTER>
+__global__ void __launch_bounds__(kListThreads, 2)
+list_adam_kernel(const __grid_constant__ AdamParams P)
+{
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t stride = gridDim.x * kListWarps;
+    uint32_t c = blockIdx.x * kListWarps + warp;
+    Piece p{};
+    if (c < P.L.pieces_n) p = load_piece(P.L.pieces + (P.L.pieces_n - 1u - c));
+    depend_on_previous();
+    const uint4 q = ld_global(reinterpret_cast<const uint4 *>(P.result));
+    const uint2 sizes = ld_global(reinterpret_cast<const uint2 *>(&P.result->step_size));
+    if (q.z != 0u) return;                             // the norm is not finite
+    const float lr = ld_global(P.lr);
+    AdamStep k{Factor{__uint_as_float(q.x), __uint_as_float(q.y)}, P.beta1, P.beta2, P.one_less_beta1, P.one_less_beta2, P.eps,
+               __uint_as_float(sizes.x), __uint_as_float(sizes.y), 0.0f};
+#pragma unroll 1
+    while (c < P.L.pieces_n) {
+        const Piece now = p;
+        c += stride;
+        if (c < P.L.pieces_n) p = load_piece(P.L.pieces + (P.L.pieces_n - 1u - c));
+        const double wd = P.decay != nullptr ? (double)ld_global(P.decay + now.tensor) : P.weight_decay;
+        k.keep = (float)(1.0 - (double)lr * wd);
+        const uint32_t type = now.len_type >> 16;
+        if (!MASTER || type == THC_F32) adam_piece<THC_F32, MASTER>(P, k, now, lane);
+        else if (type == THC_BF16) adam_piece<THC_BF16, MASTER>(P, k, now, lane);
+        else adam_piece<THC_F16, MASTER>(P, k, now, lane);
+    }
+}
+
+// ---------------------------------------------------------------------------------- addresses
+constexpr uint32_t kAssignMost = 448;
+struct AssignParams { uint64_t *to; uint32_t n; uint64_t base[kAssignMost]; };
+__global__ void list_assign_kernel(const __grid_constant__ AssignParams P)
+{
+    depend_on_previous();
+    if (threadIdx.x < P.n) P.to[threadIdx.x] = P.base[threadIdx.x];
+}
+
+}  // namespace thc
+
+// =========================================================================== host side
+using namespace thc;
+
+struct thc_tensors {
+    int device;                                // -1: host only
+    uint32_t n, count, pieces_n, sm_count;
+    uint64_t d, elements;
+    bool all_f32;
+    std::vector<uint64_t> numel, offset;
+    std::vector<uint32_t> dtype;
+    std::vector<uint64_t> address;             // [n][count]
+    struct Range { uint64_t lo, hi; uint32_t index; };
+    std::vector<Range> ranges;                 // of the tensors that are not empty, by address
+    bool overlapping;                          // tensors of the list overlap each other
+    Piece *pieces;
+    uint64_t *base;
+};
+
+static uint32_t size_of_type(uint32_t t) { return t == THC_F32 ? 4u : 2u; }
+
+// Addresses into the list: checked, sorted for the overlap checks.
+static int take_addresses(thc_tensors *h, const void *const *tensors)
+{
+    const size_t total = (size_t)h->n * h->count;
+    for (size_t i = 0; i < total; ++i) {
+        const uint64_t a = reinterpret_cast<uint64_t>(tensors[i]);
+        const uint32_t t = (uint32_t)(i % h->count);
+        if (h->numel[t] == 0) continue;
+        if (a == 0 || a % size_of_type(h->dtype[t]) != 0) return THC_EINVAL;
+    }
+    h->ranges.clear();
+    for (size_t i = 0; i < total; ++i) {
+        const uint32_t t = (uint32_t)(i % h->count);
+        h->address[i] = reinterpret_cast<uint64_t>(tensors[i]);
+        if (h->numel[t] != 0)
+            h->ranges.push_back({h->address[i], h->address[i] + h->numel[t] * size_of_type(h->dtype[t]), (uint32_t)i});
+    }
+    std::sort(h->ranges.begin(), h->ranges.end(), [](const thc_tensors::Range &a, const thc_tensors::Range &b) {
+        return a.lo != b.lo ? a.lo < b.lo : a.index < b.index;
+    });
+    h->overlapping = false;
+    uint64_t reach = 0;
+    for (const auto &r : h->ranges) {
+        if (r.lo < reach) h->overlapping = true;
+        reach = std::max(reach, r.hi);
+    }
+    return THC_OK;
+}
+
+static uint64_t base_of(const thc_tensors *h, size_t i)
+{
+    const uint32_t t = (uint32_t)(i % h->count);
+    return h->address[i] - h->offset[t] * size_of_type(h->dtype[t]);
+}
+
+int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uint64_t *numel, const uint32_t *dtype,
+                       uint32_t n, uint32_t count, thc_tensors **list)
+{
+    if (list == nullptr) return THC_EINVAL;
+    *list = nullptr;
+    if (ctx == nullptr || tensors == nullptr || numel == nullptr || dtype == nullptr) return THC_EINVAL;
+    if (n == 0 || n > THC_MAX_WORKERS || count == 0 || count > (1u << 20)) return THC_EINVAL;
+    const CtxView view = view_of(ctx);
+    if (view.device >= 0) {
+        const int rc = check_launch_ctx(ctx);
+        if (rc != THC_OK) return rc;
+    }
+    uint64_t d = 0, elements = 0, pieces_n = 0;
+    for (uint32_t t = 0; t < count; ++t) {
+        if (dtype[t] != THC_F32 && dtype[t] != THC_BF16 && dtype[t] != THC_F16) return THC_EINVAL;
+        if (numel[t] > (1ull << 40)) return THC_EINVAL;
+        elements += numel[t];
+        d += (numel[t] + THC_TENSOR_ALIGN - 1) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
+        pieces_n += (numel[t] + kPiece - 1) / kPiece;
+        if (d > (1ull << 40)) return THC_EINVAL;
+    }
+    if (elements == 0) return THC_EINVAL;
+    if (pieces_n > 0x7FFFFFFFull) return THC_EUNSUPPORTED;
+    thc_tensors *h = nullptr;
+    try {
+        h = new thc_tensors;
+        h->device = view.device;
+        h->n = n;
+        h->count = count;
+        h->pieces_n = (uint32_t)pieces_n;
+        h->sm_count = (uint32_t)view.sm_count;
+        h->d = d;
+        h->elements = elements;
+        h->all_f32 = true;
+        h->pieces = nullptr;
+        h->base = nullptr;
+        h->numel.assign(numel, numel + count);
+        h->dtype.assign(dtype, dtype + count);
+        h->offset.resize(count);
+        h->address.resize((size_t)n * count);
+        uint64_t at = 0;
+        for (uint32_t t = 0; t < count; ++t) {
+            h->offset[t] = at;
+            at += (numel[t] + THC_TENSOR_ALIGN - 1) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
+            if (dtype[t] != THC_F32 && numel[t] != 0) h->all_f32 = false;
+        }
+        const int rc = take_addresses(h, tensors);
+        if (rc != THC_OK) { delete h; return rc; }
+        if (view.device >= 0) {
+            std::vector<Piece> pieces;
+            pieces.reserve(pieces_n);
+            for (uint32_t t = 0; t < count; ++t)
+                for (uint64_t e = 0; e < numel[t]; e += kPiece)
+                    pieces.push_back({h->offset[t] + e, t, (uint32_t)std::min<uint64_t>(kPiece, numel[t] - e) | dtype[t] << 16});
+            std::vector<uint64_t> base(h->address.size());
+            for (size_t i = 0; i < base.size(); ++i) base[i] = base_of(h, i);
+            cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&h->pieces), pieces.size() * sizeof(Piece));
+            if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&h->base), base.size() * sizeof(uint64_t));
+            if (e == cudaSuccess) e = cudaMemcpy(h->pieces, pieces.data(), pieces.size() * sizeof(Piece), cudaMemcpyHostToDevice);
+            if (e == cudaSuccess) e = cudaMemcpy(h->base, base.data(), base.size() * sizeof(uint64_t), cudaMemcpyHostToDevice);
+            if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);   // a copy from pageable memory may still be on its way
+            if (e != cudaSuccess) {
+                thc_tensors_destroy(h);
+                return cuda_fail(e);
+            }
+        }
+    } catch (const std::bad_alloc &) {
+        thc_tensors_destroy(h);
+        return THC_EINVAL;
+    }
+    *list = h;
+    return THC_OK;
+}
+
+int thc_tensors_destroy(thc_tensors *h)
+{
+    if (h == nullptr) return THC_OK;
+    if (h->pieces != nullptr) cudaFree(h->pieces);
+    if (h->base != nullptr) cudaFree(h->base);
+    delete h;
+    return THC_OK;
+}
+
+// CTAs per worker of a launch over all pieces.
+static uint32_t ctas_of(const thc_tensors *h, uint32_t per_sm)
+{
+    const uint32_t most = std::max(1u, h->sm_count * per_sm / h->n);
+    return std::min(most, (h->pieces_n + kListWarps - 1) / kListWarps);
+}
+
+static uint64_t round_up256(uint64_t v) { return (v + 255) / 256 * 256; }
+
+// Workspace: results of the workers, then the partial sums.
+static uint64_t workspace_need(const thc_tensors *h)
+{
+    return round_up256(h->n * sizeof(NormResult)) + round_up256((uint64_t)h->n * ctas_of(h, kNormCtasPerSm) * sizeof(double));
+}
+
+int thc_tensors_sizes(const thc_tensors *h, thc_tensors_sizes_t *s)
+{
+    if (h == nullptr || s == nullptr) return THC_EINVAL;
+    memset(s, 0, sizeof *s);
+    s->d = h->d;
+    s->elements = h->elements;
+    s->workspace_bytes = workspace_need(h);
+    s->n = h->n;
+    s->count = h->count;
+    s->device = h->device;
+    return THC_OK;
+}
+
+int thc_tensors_offsets(const thc_tensors *h, uint64_t *offsets)
+{
+    if (h == nullptr || offsets == nullptr) return THC_EINVAL;
+    std::copy(h->offset.begin(), h->offset.end(), offsets);
+    return THC_OK;
+}
+
+// A list can be used where its context can launch.
+static int check_list(const thc_ctx *ctx, const thc_tensors *h)
+{
+    if (ctx == nullptr || h == nullptr) return THC_EINVAL;
+    const int rc = check_launch_ctx(ctx);
+    if (rc != THC_OK) return rc;
+    return h->device == view_of(ctx).device ? THC_OK : THC_EINVAL;
+}
+
+int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *h, const void *const *tensors, void *stream)
+{
+    int rc = check_list(ctx, h);
+    if (rc != THC_OK) return rc;
+    if (tensors == nullptr) return THC_EINVAL;
+    try {
+        std::vector<uint64_t> old_address = h->address;
+        std::vector<thc_tensors::Range> old_ranges = h->ranges;
+        const bool old_overlapping = h->overlapping;
+        rc = take_addresses(h, tensors);
+        for (size_t i = 0; rc == THC_OK && i < h->address.size(); i += kAssignMost) {
+            AssignParams P;
+            P.to = h->base + i;
+            P.n = (uint32_t)std::min<size_t>(kAssignMost, h->address.size() - i);
+            for (uint32_t j = 0; j < P.n; ++j) P.base[j] = base_of(h, i + j);
+            const cudaError_t e = launch_after(list_assign_kernel, dim3(1), (kAssignMost + 31) / 32 * 32, 0, static_cast<cudaStream_t>(stream), P);
+            if (e != cudaSuccess) return cuda_fail(e);
+        }
+        if (rc != THC_OK) {
+            h->address.swap(old_address);
+            h->ranges.swap(old_ranges);
+            h->overlapping = old_overlapping;
+        }
+    } catch (const std::bad_alloc &) {
+        return THC_EINVAL;
+    }
+    return rc;
+}
+
+static ListTable table_of(const thc_tensors *h) { return ListTable{h->pieces, h->base, h->count, h->pieces_n}; }
+
+static int check_workspace(const thc_tensors *h, const void *workspace, uint64_t bytes)
+{
+    if (workspace == nullptr || !aligned16(workspace)) return THC_EINVAL;
+    return bytes < workspace_need(h) ? THC_EWORKSPACE : THC_OK;
+}
+
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Whether [lo, hi) overlaps a tensor of the list.  Tensors that overlap each other make the answer "yes" at most
+// more often than it is.
+static bool overlaps(const thc_tensors *h, uint64_t lo, uint64_t hi)
+{
+    if (h->overlapping) {
+        for (const auto &r : h->ranges) if (r.lo < hi && lo < r.hi) return true;
+        return false;
+    }
+    const auto it = std::lower_bound(h->ranges.begin(), h->ranges.end(), lo, [](const thc_tensors::Range &r, uint64_t a) { return r.hi <= a; });
+    return it != h->ranges.end() && it->lo < hi;
+}
+
+static NormOut norm_out(const CtxView &v, const thc_tensors *h, double max_norm, float *norms, void *workspace)
+{
+    NormOut o;
+    memset(&o, 0, sizeof o);
+    o.result = static_cast<NormResult *>(workspace);
+    o.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + round_up256(h->n * sizeof(NormResult)));
+    o.norms = norms;
+    o.dev = v.dev;
+    o.max_norm = max_norm;
+    return o;
+}
+
+static int launch_norm(const thc_tensors *h, const NormOut &o, const void *flat, cudaStream_t st)
+{
+    THC_CUDA(launch_after(list_norm_kernel, dim3(ctas_of(h, kNormCtasPerSm), h->n), kListThreads, 0, st, table_of(h), o,
+                          reinterpret_cast<uint64_t>(flat)));
+    return THC_OK;
+}
+
+int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    if (norms == nullptr || !aligned4(norms)) return THC_EINVAL;
+    if ((rc = check_workspace(list, workspace, workspace_bytes)) != THC_OK) return rc;
+    return launch_norm(list, norm_out(view_of(ctx), list, INFINITY, norms, workspace), nullptr, static_cast<cudaStream_t>(stream));
+}
+
+// Norm (unless there is nothing to form from it), then the products.
+static int launch_move(thc_ctx *ctx, void (*kern)(MoveParams), MoveParams &P, const thc_tensors *h, const void *flat, double max_norm,
+                       float *norms, void *workspace, cudaStream_t st)
+{
+    P.result = nullptr;
+    if (norms != nullptr) {
+        const NormOut o = norm_out(view_of(ctx), h, max_norm, norms, workspace);
+        const int rc = launch_norm(h, o, flat, st);
+        if (rc != THC_OK) return rc;
+        P.result = o.result;
+    }
+    THC_CUDA(launch_after(kern, dim3(ctas_of(h, kMoveCtasPerSm), h->n), kListThreads, 0, st, P));
+    return THC_OK;
+}
+
+// max_norm, norms and workspace of a call that clips.
+static int check_clip(const thc_tensors *h, double max_norm, const float *norms, bool need_norms, const void *workspace, uint64_t bytes)
+{
+    if (!(max_norm >= 0.0) || !aligned4(norms)) return THC_EINVAL;
+    if (norms == nullptr) return need_norms || !isinf(max_norm) ? THC_EINVAL : THC_OK;
+    return check_workspace(h, workspace, bytes);
+}
+
+int thc_clip_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const thc_tensors *out_or_null, float *norms,
+                   void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    const thc_tensors *out = out_or_null != nullptr ? out_or_null : list;
+    if ((rc = check_list(ctx, out)) != THC_OK) return rc;
+    if ((rc = check_clip(list, max_norm, norms, true, workspace, workspace_bytes)) != THC_OK) return rc;
+    if (out->n != list->n || out->numel != list->numel || out->dtype != list->dtype || out->overlapping) return THC_EINVAL;
+    if (out != list) {
+        for (const auto &r : list->ranges) {
+            if (out->address[r.index] == r.lo) {
+                // its own place, and as tensors of `out` do not overlap each other, no other one's
+                continue;
+            }
+            if (overlaps(out, r.lo, r.hi)) return THC_EINVAL;
+        }
+    }
+    MoveParams P;
+    memset(&P, 0, sizeof P);
+    P.src = table_of(list);
+    P.dst = table_of(out);
+    return launch_move(ctx, list_move_kernel<kClip>, P, list, nullptr, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *const *ef_or_null, void *const *flats,
+                     float *norms, void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    if ((rc = check_clip(list, max_norm, norms, false, workspace, workspace_bytes)) != THC_OK) return rc;
+    const bool bf16 = view_of(ctx).in_dtype == THC_BF16;
+    if (bf16 && ef_or_null != nullptr) return THC_EUNSUPPORTED;
+    if (flats == nullptr) return THC_EINVAL;
+    const uint64_t bytes = list->d * (bf16 ? 2u : 4u);
+    MoveParams P;
+    memset(&P, 0, sizeof P);
+    for (uint32_t i = 0; i < list->n; ++i) {
+        if (flats[i] == nullptr || !aligned16(flats[i])) return THC_EINVAL;
+        P.dst_flat[i] = reinterpret_cast<uint64_t>(flats[i]);
+        if (ef_or_null != nullptr) {
+            if (ef_or_null[i] == nullptr || !aligned16(ef_or_null[i])) return THC_EINVAL;
+            P.ef[i] = reinterpret_cast<uint64_t>(ef_or_null[i]);
+        }
+    }
+    const auto apart = [bytes](uint64_t a, uint64_t b) { return a + bytes <= b || b + bytes <= a; };
+    for (uint32_t i = 0; i < list->n; ++i) {
+        if (overlaps(list, P.dst_flat[i], P.dst_flat[i] + bytes)) return THC_EINVAL;
+        for (uint32_t j = 0; j < list->n; ++j) {
+            if (j != i && !apart(P.dst_flat[i], P.dst_flat[j])) return THC_EINVAL;
+            if (ef_or_null != nullptr && !(j == i && P.ef[j] == P.dst_flat[i]) && !apart(P.dst_flat[i], P.ef[j])) return THC_EINVAL;
+        }
+    }
+    P.src = table_of(list);
+    return launch_move(ctx, ef_or_null != nullptr ? list_move_kernel<kGatherResidual> : bf16 ? list_move_kernel<kGatherBf16> : list_move_kernel<kGatherF32>,
+                       P, list, nullptr, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const thc_tensors *list, float *norms, void *workspace,
+                      uint64_t workspace_bytes, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    if ((rc = check_clip(list, max_norm, norms, false, workspace, workspace_bytes)) != THC_OK) return rc;
+    if (flat == nullptr || !aligned16(flat) || list->n != 1 || list->overlapping) return THC_EINVAL;
+    const uint64_t lo = reinterpret_cast<uint64_t>(flat), hi = lo + list->d * 4u;
+    for (const auto &r : list->ranges)
+        if (r.lo < hi && lo < r.hi && !(list->dtype[r.index] == THC_F32 && r.lo == lo + list->offset[r.index] * 4u)) return THC_EINVAL;
+    MoveParams P;
+    memset(&P, 0, sizeof P);
+    P.dst = table_of(list);
+    P.src_flat = lo;
+    return launch_move(ctx, list_move_kernel<kScatter>, P, list, flat, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int thc_adamw(thc_ctx *ctx, const thc_adamw_config *cfg, const float *grad, const thc_tensors *list, const float *lr, int64_t *step,
+              float *master_or_null, float *m, float *v, const float *decay_or_null, float *norms, void *workspace,
+              uint64_t workspace_bytes, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    if (cfg == nullptr) return THC_EINVAL;
+    if ((rc = check_clip(list, cfg->max_norm, norms, true, workspace, workspace_bytes)) != THC_OK) return rc;
+    if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return THC_EINVAL;
+    if (!(cfg->eps >= 0.0) || isinf(cfg->eps) || !(cfg->weight_decay >= 0.0) || isinf(cfg->weight_decay)) return THC_EINVAL;
+    if (list->n != 1 || list->overlapping || (master_or_null == nullptr && !list->all_f32)) return THC_EINVAL;
+    if (lr == nullptr || !aligned4(lr) || step == nullptr || (reinterpret_cast<uintptr_t>(step) & 7u) != 0 || !aligned4(decay_or_null)) return THC_EINVAL;
+    const void *flat[4] = {grad, m, v, master_or_null};
+    const uint64_t bytes = list->d * 4u;
+    const int flats = master_or_null != nullptr ? 4 : 3;
+    for (int i = 0; i < flats; ++i) {
+        if (flat[i] == nullptr || !aligned16(flat[i])) return THC_EINVAL;
+        const uint64_t a = reinterpret_cast<uint64_t>(flat[i]);
+        if (overlaps(list, a, a + bytes)) return THC_EINVAL;
+        for (int j = 0; j < i; ++j) {
+            const uint64_t b = reinterpret_cast<uint64_t>(flat[j]);
+            if (a < b + bytes && b < a + bytes) return THC_EINVAL;
+        }
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    NormOut o = norm_out(view_of(ctx), list, cfg->max_norm, norms, workspace);
+    o.lr = lr;
+    o.step = step;
+    o.beta1 = cfg->beta1;
+    o.beta2 = cfg->beta2;
+    if ((rc = launch_norm(list, o, grad, st)) != THC_OK) return rc;
+    AdamParams P;
+    memset(&P, 0, sizeof P);
+    P.L = table_of(list);
+    P.result = o.result;
+    P.grad = grad;
+    P.master = master_or_null;
+    P.m = m;
+    P.v = v;
+    P.lr = lr;
+    P.decay = decay_or_null;
+    P.beta1 = (float)cfg->beta1;
+    P.beta2 = (float)cfg->beta2;
+    P.one_less_beta1 = (float)(1.0 - cfg->beta1);
+    P.one_less_beta2 = (float)(1.0 - cfg->beta2);
+    P.eps = (float)cfg->eps;
+    P.weight_decay = cfg->weight_decay;
+    const dim3 grid(ctas_of(list, 2));
+    if (master_or_null != nullptr) THC_CUDA(launch_after(list_adam_kernel<true>, grid, kListThreads, 0, st, P));
+    else THC_CUDA(launch_after(list_adam_kernel<false>, grid, kListThreads, 0, st, P));
+    return THC_OK;
+}

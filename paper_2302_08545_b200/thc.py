@@ -8,6 +8,7 @@ missing the import of the library fails loudly -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
@@ -17,13 +18,16 @@ _lib = None
 _native = None
 
 THC_OK, THC_EINVAL, THC_EUNSUPPORTED, THC_ECUDA, THC_EWORKSPACE = 0, -1, -2, -3, -4
-THC_F32, THC_BF16 = 0, 1
+THC_F32, THC_BF16, THC_F16 = 0, 1, 2
+TENSOR_ALIGN = 64
 THC_MAX_WORKERS = 64
 STATUS_NONFINITE, STATUS_ZERO_BLOCK, STATUS_WAIT_TIMEOUT = 1, 2, 4
 
 EXPORTS = ("thc_create", "thc_destroy", "thc_sizes", "thc_prepare", "thc_compress",
            "thc_quantize_rotated", "thc_aggregate", "thc_decompress", "thc_aggregate_decompress", "thc_prepare_noalloc",
-           "thc_error_feedback", "thc_accumulate_error", "thc_prepare_compress", "thc_prepare_minmax", "thc_debug_skip_tasks", "thc_status", "thc_strerror", "thc_version")
+           "thc_error_feedback", "thc_accumulate_error", "thc_prepare_compress", "thc_prepare_minmax",
+           "thc_tensors_create", "thc_tensors_destroy", "thc_tensors_sizes", "thc_tensors_offsets", "thc_tensors_assign",
+           "thc_grad_norm", "thc_clip_grads", "thc_gather_grads", "thc_scatter_grads", "thc_adamw", "thc_debug_skip_tasks", "thc_status", "thc_strerror", "thc_version")
 NOALLOC_SCRATCH_BYTES = 4 << 20
 
 
@@ -39,6 +43,16 @@ class _Config(ctypes.Structure):
                 ("log2_block", ctypes.c_uint32), ("seed", ctypes.c_uint64),
                 ("in_dtype", ctypes.c_uint32), ("workers", ctypes.c_uint32),
                 ("acc_bits", ctypes.c_uint32), ("range_mode", ctypes.c_uint32)]
+
+
+class _TensorsSizes(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_uint64), ("elements", ctypes.c_uint64), ("workspace_bytes", ctypes.c_uint64),
+                ("n", ctypes.c_uint32), ("count", ctypes.c_uint32), ("device", ctypes.c_int32)]
+
+
+class _AdamwConfig(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("max_norm", ctypes.c_double)]
 
 
 class _Sizes(ctypes.Structure):
@@ -87,6 +101,17 @@ def lib():
     L.thc_prepare_compress.argtypes = [vp, pp, u32, u32, u64, u32, vp, pp, pp, vp, u64, vp]
     L.thc_error_feedback.argtypes = [vp, pp, pp, u32, u64, u32, vp, pp, vp, u64, vp]
     L.thc_accumulate_error.argtypes = [vp, pp, pp, u32, u64, vp]
+    pu64, pu32, f64 = ctypes.POINTER(u64), ctypes.POINTER(u32), ctypes.c_double
+    L.thc_tensors_create.argtypes = [vp, pp, pu64, pu32, u32, u32, pp]
+    L.thc_tensors_destroy.argtypes = [vp]
+    L.thc_tensors_sizes.argtypes = [vp, ctypes.POINTER(_TensorsSizes)]
+    L.thc_tensors_offsets.argtypes = [vp, pu64]
+    L.thc_tensors_assign.argtypes = [vp, vp, pp, vp]
+    L.thc_grad_norm.argtypes = [vp, vp, vp, vp, u64, vp]
+    L.thc_clip_grads.argtypes = [vp, vp, f64, vp, vp, vp, u64, vp]
+    L.thc_gather_grads.argtypes = [vp, vp, f64, pp, pp, vp, vp, u64, vp]
+    L.thc_scatter_grads.argtypes = [vp, vp, f64, vp, vp, vp, u64, vp]
+    L.thc_adamw.argtypes = [vp, ctypes.POINTER(_AdamwConfig), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     L.thc_debug_skip_tasks.argtypes = [vp, u32]
     L.thc_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32), vp]
     for name in EXPORTS[:-2]:
@@ -142,6 +167,92 @@ def prepare_noalloc(grads, d: int, log2_block: int, in_dtype: int, t_p: float, s
            "thc_prepare_noalloc")
 
 
+class Tensors:
+    """A list of tensors (``thc_tensors``): for each of n workers the same number of contiguous float32,
+    bfloat16 or float16 tensors, of the same sizes and types for every worker.  Keeps the tensors.
+
+    ``workers`` is a sequence of n sequences of tensors.  In a flat vector of ``d`` elements tensor t
+    starts at ``offsets[t]``; ``views(flat)`` are the tensors' places in it.  ``workspace_bytes`` is what
+    the calls that take the list need.  A tensor that is later given other memory (``set_``, a new
+    ``.grad``) is not followed: ``assign`` takes the new ones."""
+
+    _CODES = None
+
+    def __init__(self, ctx: "Context", workers):
+        self._h = ctypes.c_void_p()
+        self._handle = 0
+        self._ctx = ctx
+        workers = [list(w) for w in workers]
+        if not workers or not workers[0]:
+            raise ValueError("a list has at least one worker with one tensor")
+        self.shapes = [tuple(t.shape) for t in workers[0]]
+        self.dtypes = [t.dtype for t in workers[0]]
+        codes = self._codes()
+        for t in self.dtypes:
+            if t not in codes:
+                raise ValueError(f"tensors of type {t} are not served")
+        self.n, self.count = len(workers), len(workers[0])
+        addresses = self._addresses(workers)
+        numel = (ctypes.c_uint64 * self.count)(*[t.numel() for t in workers[0]])
+        kinds = (ctypes.c_uint32 * self.count)(*[codes[t] for t in self.dtypes])
+        _check(lib().thc_tensors_create(ctx._h, addresses, numel, kinds, self.n, self.count, ctypes.byref(self._h)),
+               "thc_tensors_create")
+        s = _TensorsSizes()
+        _check(lib().thc_tensors_sizes(self._h, ctypes.byref(s)), "thc_tensors_sizes")
+        self.d, self.elements, self.workspace_bytes, self.device = s.d, s.elements, s.workspace_bytes, s.device
+        at = (ctypes.c_uint64 * self.count)()
+        _check(lib().thc_tensors_offsets(self._h, at), "thc_tensors_offsets")
+        self.offsets = list(at)
+        self._check_device(workers)
+        self.tensors = workers
+        self._handle = self._h.value
+
+    @classmethod
+    def _codes(cls):
+        if cls._CODES is None:
+            import torch
+            Tensors._CODES = {torch.float32: THC_F32, torch.bfloat16: THC_BF16, torch.float16: THC_F16}
+        return cls._CODES
+
+    def _addresses(self, workers):
+        if len(workers) != self.n or any(len(w) != self.count for w in workers):
+            raise ValueError("every worker has the same number of tensors")
+        for w in workers:
+            for t, shape, dtype in zip(w, self.shapes, self.dtypes):
+                if tuple(t.shape) != shape or t.dtype != dtype:
+                    raise ValueError("the workers' tensors differ in shape or type")
+                if not t.is_contiguous():
+                    raise ValueError("tensors of a list are contiguous")
+        return (ctypes.c_void_p * (self.n * self.count))(*[t.data_ptr() for w in workers for t in w])
+
+    def _check_device(self, workers):
+        if any(t.get_device() != self.device for w in workers for t in w):
+            raise ValueError("tensors of a list are on the context's device")
+
+    def assign(self, workers, stream=None):
+        """Other tensors of the same shapes and types, for the calls issued on ``stream`` from here on."""
+        workers = [list(w) for w in workers]
+        addresses = self._addresses(workers)
+        self._check_device(workers)
+        _check(lib().thc_tensors_assign(self._ctx._h, self._h, addresses, _stream(stream)), "thc_tensors_assign")
+        self.tensors = workers
+
+    def views(self, flat):
+        return [flat[o: o + math.prod(s)].view(s) for o, s in zip(self.offsets, self.shapes)]
+
+    def close(self):
+        if self._h.value:
+            lib().thc_tensors_destroy(self._h)
+            self._h = ctypes.c_void_p()
+            self._handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class Context:
     """Owns a ``thc_ctx``.  Methods mirror the C entry points one to one."""
 
@@ -158,7 +269,7 @@ class Context:
         self._h = ctypes.c_void_p()
         _check(lib().thc_create(ctypes.byref(cfg), ctypes.byref(self._h)), "thc_create")
         self.bits, self.granularity, self.log2_block = bits, granularity, log2_block
-        self.workers = workers
+        self.workers, self.in_dtype = workers, in_dtype
         self._handle = self._h.value
         self._call = _binding()
 
@@ -221,6 +332,36 @@ class Context:
 
     def accumulate_error(self, grads, ef, d: int, stream=None):
         _check(self._call.accumulate_error(self._handle, grads, ef, d, stream), "thc_accumulate_error")
+
+    # -- lists of tensors; norms: float32, one per worker
+    def grad_norm(self, tensors: Tensors, norms, workspace, stream=None):
+        """The global L2 norm of each worker's tensors."""
+        _check(self._call.grad_norm(self._handle, tensors._handle, norms, workspace, stream), "thc_grad_norm")
+
+    def clip_grads(self, tensors: Tensors, max_norm: float, norms, workspace, out: Tensors | None = None, stream=None):
+        """Each worker's tensors times min(1, max_norm / (norm + 1e-6)), in place or into `out`."""
+        if out is not None and not out._handle:
+            raise ValueError("`out` is closed")
+        _check(self._call.clip_grads(self._handle, tensors._handle, max_norm, None if out is None else out._handle,
+                                     norms, workspace, stream), "thc_clip_grads")
+
+    def gather_grads(self, tensors: Tensors, max_norm: float, flats, norms, workspace, ef=None, stream=None):
+        """Each worker's tensors, clipped, to its flat vector, plus its residual `ef`.  max_norm = math.inf
+        and norms = None: as they are."""
+        _check(self._call.gather_grads(self._handle, tensors._handle, max_norm, ef, flats, norms, workspace,
+                                       self.in_dtype == THC_BF16, stream), "thc_gather_grads")
+
+    def scatter_grads(self, flat, max_norm: float, tensors: Tensors, norms, workspace, stream=None):
+        """The flat average, clipped, to the tensors."""
+        _check(self._call.scatter_grads(self._handle, flat, max_norm, tensors._handle, norms, workspace, stream),
+               "thc_scatter_grads")
+
+    def adamw(self, grad, tensors: Tensors, lr, step, m, v, norms, workspace, master=None, decay=None, betas=(0.9, 0.999),
+              eps: float = 1e-8, weight_decay: float = 0.0, max_norm: float = math.inf, stream=None):
+        """The Adam step with decoupled weight decay on the flat average, clipped; `lr` (float32) and `step`
+        (int64) are one-element tensors on the device, `decay` is one weight decay per tensor."""
+        _check(self._call.adamw(self._handle, (betas[0], betas[1], eps, weight_decay, max_norm), grad, tensors._handle, lr,
+                                step, master, m, v, decay, norms, workspace, stream), "thc_adamw")
 
     def debug_skip_tasks(self, count: int):
         """Test hook: the next pipeline launch starts its task queue at `count`."""

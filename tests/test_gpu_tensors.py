@@ -1,0 +1,436 @@
+"""Lists of tensors on the GPU: norm, clipping, the ways into and out of the flat vector and the Adam step against
+their definitions in 64 bits.
+
+Bounds: the norm is an fp64 sum rounded to fp32 (one rounding, u = 2^-24); the factor is formed in fp64 and rounded
+(u), the product is rounded (u), then once more to the tensor's type.  The Adam step's are beside its test."""
+import math
+
+import pytest
+import torch
+
+import tensor_lists as T
+from tensor_lists import U
+
+pytestmark = pytest.mark.gpu
+
+EDGES = [1, 7, 0, 8, 9, 63, 64, 65, 255, 1000, 2047, 2048, 2049, 4096 + 17, 100_003]
+SMALL = 1.0 + 2.0 ** -16               # second-order terms of the bounds
+
+
+def context(in_dtype="f32", **kw):
+    from paper_2302_08545_b200 import thc, workloads as W
+    return thc.Context(**dict(dict(bits=4, granularity=30, table=W.TABLES[(4, 30)], t_p=2.0, log2_block=12, seed=1,
+                                   in_dtype=thc.THC_BF16 if in_dtype == "bf16" else thc.THC_F32), **kw))
+
+
+def setup(workers, in_dtype="f32"):
+    from paper_2302_08545_b200 import thc
+    ctx = context(in_dtype)
+    lst = thc.Tensors(ctx, workers)
+    norms = torch.full((lst.n,), -1.0, device="cuda")
+    ws = torch.empty(lst.workspace_bytes, dtype=torch.uint8, device="cuda")
+    return ctx, lst, norms, ws
+
+
+def check_norms(norms, workers):
+    ref = torch.tensor([T.norm(w) for w in workers], dtype=torch.float64)
+    T.within(norms.cpu(), ref, ref * U * SMALL)
+    return ref.tolist()
+
+
+LISTS = [
+    ([1], ["f32"], 1, 0), ([1], ["f16"], 3, 1), ([5], ["bf16"], 1, 3), (EDGES, ["f32"], 1, 0), (EDGES, ["bf16"], 2, 0),
+    (EDGES, ["f16"], 1, 0), (EDGES, ["f32", "bf16", "f16", "bf16"], 3, 0), (EDGES, ["f32"], 2, 1), (EDGES, ["bf16"], 1, 4),
+    (EDGES, ["f16"], 2, 2), (EDGES, ["f16", "f32"], 1, 5), ([300_001, 2_000_003], ["f32"], 5, 0), ([7_000_003], ["bf16"], 1, 0),
+    ([17] * 400, ["f32", "bf16"], 2, 0), ([4096] * 64, ["bf16"], 64, 0),
+]
+
+
+@pytest.mark.parametrize("sizes,types,n,shift", LISTS)
+def test_norm(sizes, types, n, shift):
+    workers = T.make(sizes, types, n, shift, seed=len(sizes) + n)
+    ctx, lst, norms, ws = setup(workers)
+    ws.fill_(0xA5)
+    ctx.grad_norm(lst, norms, ws)
+    check_norms(norms, workers)
+    first = norms.clone()
+    ctx.grad_norm(lst, norms, ws)
+    assert torch.equal(first, norms) and ctx.status() == 0
+
+
+@pytest.mark.parametrize("sizes,types,n,shift", LISTS)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clip(sizes, types, n, shift, in_place):
+    from paper_2302_08545_b200 import thc
+    workers = T.make(sizes, types, n, shift, seed=3)
+    before = [[x.clone() for x in w] for w in workers]
+    ctx, lst, norms, ws = setup(workers)
+    most = 0.7 * T.norm(workers[0])        # clips some workers or all
+    outs = workers if in_place else T.make(sizes, types, n, shift + 1 if shift else 0, seed=9)
+    ctx.clip_grads(lst, most, norms, ws, out=None if in_place else thc.Tensors(ctx, outs))
+    ref = check_norms(norms, before)
+    for w, o, r in zip(before, outs, ref):
+        c = T.factor(r, most)
+        for x, y in zip(w, o):
+            exact = x.double() * c
+            rel, least = T.half_step(y.dtype)
+            T.within(y, exact, exact.abs() * ((2 * U + (rel if y.dtype != torch.float32 else 0)) * SMALL) + least + 2.0 ** -149)
+    if not in_place:
+        for w, b in zip(workers, before):
+            assert all(torch.equal(x, y) for x, y in zip(w, b))
+
+
+def test_clip_leaves_what_is_around_the_tensors_alone():
+    room = torch.full((20_000,), 5.0, dtype=torch.bfloat16, device="cuda")
+    pieces, at = [], 3
+    for s in (1, 9, 2047, 4099, 64, 5):
+        pieces.append(room[at: at + s])
+        at += s + 2
+    ctx, lst, norms, ws = setup([pieces])
+    ctx.clip_grads(lst, 1.0, norms, ws)
+    inside = torch.zeros_like(room, dtype=torch.bool)
+    for p in pieces:
+        inside[p.storage_offset(): p.storage_offset() + p.numel()] = True
+    assert bool((room[~inside] == 5.0).all()) and bool((room[inside] < 5.0).all())
+
+
+@pytest.mark.parametrize("below", [True, False])
+def test_a_norm_below_the_bound_changes_nothing(below):
+    workers = T.make(EDGES, ["f32", "bf16", "f16"], 2, seed=4)
+    before = [[x.clone() for x in w] for w in workers]
+    ctx, lst, norms, ws = setup(workers)
+    ctx.clip_grads(lst, 1e9 if below else math.inf, norms, ws)
+    assert all(torch.equal(x, y) for w, b in zip(workers, before) for x, y in zip(w, b))
+    check_norms(norms, before)
+
+
+def test_max_norm_zero_and_zero_gradients():
+    workers = T.make([100, 3000], ["f32"], 1, seed=4)
+    ctx, lst, norms, ws = setup(workers)
+    ctx.clip_grads(lst, 0.0, norms, ws)
+    assert all(not bool(x.any()) for x in workers[0])
+    ctx.clip_grads(lst, 1.0, norms, ws)
+    assert float(norms) == 0.0 and all(not bool(x.any()) for x in workers[0]) and ctx.status() == 0
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_values_that_are_not_finite(value):
+    from paper_2302_08545_b200 import thc
+    workers = T.make([100, 5000], ["f32", "bf16"], 3, seed=4)
+    workers[1][1][4321] = value
+    before = [[x.clone() for x in w] for w in workers]
+    ctx, lst, norms, ws = setup(workers)
+    ctx.clip_grads(lst, 1.0, norms, ws)
+    assert ctx.status() == thc.STATUS_NONFINITE and ctx.status() == 0
+    got = norms.tolist()
+    assert math.isfinite(got[0]) and math.isfinite(got[2]) and (math.isnan(got[1]) if math.isnan(value) else got[1] == math.inf)
+    for x, y in zip(workers[1], before[1]):
+        if math.isnan(value):
+            assert bool(torch.isnan(x).all())
+        else:
+            assert torch.equal(torch.isnan(x), torch.isinf(y)) and not bool(x[~torch.isnan(x)].any())
+    for i in (0, 2):
+        assert all(bool(torch.isfinite(x).all()) for x in workers[i])
+
+
+def test_values_whose_squares_leave_fp32():
+    """3e38 and 1e-30: their squares are neither in fp32's range; fp64 holds them."""
+    x = torch.full((5000,), 1e-30, device="cuda")
+    ctx, lst, norms, ws = setup([[x]])
+    ctx.clip_grads(lst, 1.0, norms, ws)
+    check_norms(norms, [[torch.full((5000,), 1e-30)]])
+    x.fill_(3e38)
+    y = x.clone()
+    ctx.clip_grads(lst, 2.0, norms, ws)
+    assert math.isinf(float(norms)) and ctx.status() == 0      # past fp32, not past fp64
+    exact = y.double() * (2.0 / (math.sqrt(5000) * float(y[0].double()) + 1e-6))
+    T.within(x, exact, exact.abs() * 2 * U * SMALL)
+
+
+@pytest.mark.parametrize("flat", ["f32", "bf16", "residual", "residual in place"])
+@pytest.mark.parametrize("sizes,types,n,shift", LISTS)
+def test_gather(sizes, types, n, shift, flat):
+    workers = T.make(sizes, types, n, shift, seed=5)
+    ctx, lst, norms, ws = setup(workers, "bf16" if flat == "bf16" else "f32")
+    most = 0.7 * T.norm(workers[0])
+    dt = torch.bfloat16 if flat == "bf16" else torch.float32
+    room = torch.full((n, lst.d + 64), 7.0, device="cuda", dtype=dt)
+    flats = [row[: lst.d] for row in room]
+    ef, e64 = None, [torch.zeros(lst.d, dtype=torch.float64, device="cuda")] * n
+    if flat.startswith("residual"):
+        ef = flats if flat.endswith("place") else [torch.empty(lst.d, device="cuda") for _ in range(n)]
+        for e in ef:
+            e.normal_()
+        e64 = [e.double() for e in ef]
+    ctx.gather_grads(lst, most, flats, norms, ws, ef=ef)
+    ref = check_norms(norms, workers)
+    for w, y, e, r in zip(workers, flats, e64, ref):
+        c = T.factor(r, most)
+        exact, product = e.clone(), torch.zeros_like(e)
+        for x, o, v in zip(w, lst.offsets, lst.views(product)):
+            v.copy_(x.double() * c)
+        exact += product
+        rel = T.half_step(dt)[0]
+        # factor: u of the product; one rounding of the result (fp32: of the product or of the fused sum)
+        bound = product.abs() * U + exact.abs() * (U + (rel if flat == "bf16" else 0))
+        T.within(y, exact, bound * SMALL + 2.0 ** -149)
+        T.within(y[product == 0], e[product == 0], torch.zeros_like(e[product == 0]))
+    assert bool((room[:, lst.d:] == 7.0).all())
+
+
+def test_gather_without_clipping_is_a_copy():
+    workers = T.make(EDGES, ["f32", "f16"], 2, seed=5)
+    ctx, lst, norms, ws = setup(workers)
+    flats = [torch.full((lst.d,), 3.0, device="cuda") for _ in range(2)]
+    ctx.gather_grads(lst, math.inf, flats, None, None)
+    for w, f in zip(workers, flats):
+        assert all(torch.equal(x.float(), v) for x, v in zip(w, lst.views(f)))
+        inside = torch.zeros(lst.d, dtype=torch.bool, device="cuda")
+        for v in lst.views(inside):
+            v.fill_(True)
+        assert not bool(f[~inside].any())
+    workers[0][3][0] = math.nan            # no norm: other elements are not touched by it
+    ctx.gather_grads(lst, math.inf, flats, None, None)
+    assert int(torch.isnan(flats[0]).sum()) == 1 and ctx.status() == 0
+
+
+@pytest.mark.parametrize("sizes,types,n,shift", [c for c in LISTS if c[2] < 5])
+def test_scatter(sizes, types, n, shift):
+    workers = T.make(sizes, types, 1, shift, seed=6)
+    ctx, lst, norms, ws = setup(workers)
+    flat = torch.randn(lst.d, device="cuda")
+    before = flat.clone()
+    views = lst.views(flat)
+    most = 0.5 * T.norm(views)
+    ctx.scatter_grads(flat, most, lst, norms, ws)
+    r, = check_norms(norms, [views])       # what is between the tensors does not count
+    for x, v in zip(workers[0], views):
+        exact = v.double() * T.factor(r, most)
+        rel, least = T.half_step(x.dtype)
+        T.within(x, exact, exact.abs() * ((2 * U + (rel if x.dtype != torch.float32 else 0)) * SMALL) + least + 2.0 ** -149)
+    assert torch.equal(flat, before)
+    ctx.scatter_grads(flat, math.inf, lst, None, None)
+    assert all(torch.equal(x, v.to(x.dtype)) for x, v in zip(workers[0], views))
+
+
+def test_scatter_to_places_in_the_flat_vector_itself():
+    from paper_2302_08545_b200 import thc
+    sizes = [100, 5000, 63]
+    ctx, lst, norms, ws = setup(T.make(sizes, ["f32"], 1))
+    flat = torch.randn(lst.d, device="cuda")
+    before = flat.clone()
+    own = thc.Tensors(ctx, [lst.views(flat)])
+    ctx.scatter_grads(flat, 1.0, own, norms, ws)
+    r, = check_norms(norms, [lst.views(before)])
+    exact = before.double()
+    for v in lst.views(exact):
+        v.mul_(T.factor(r, 1.0))
+    T.within(flat, exact, exact.abs() * 2 * U * SMALL)
+
+
+def adam_exact(g, m, v, w, c, t, lr, wd, b1, b2, eps):
+    """The step in 64 bits and bounds for m, v, w.  With u per rounding and per rounded constant: g = c x is 2 u off;
+    m = fma(b1, m, a1 g): u |b1 m| (b1) + 4 u |a1 g| (g, a1, product) + u |m|.  v is a sum of positive terms, the larger
+    error of which is a2 g g with 2 x 2 u (g), u (a2), 2 u (products): at most 7 u v + u v.  The denominator's root has half of
+    v's and its own (5 u), its factor u, eps u, the sum u: at most 8 u.  The quotient adds 1 u and m's own error, the step
+    size 1 u; keep = 1 - lr wd and its product 2 u |w|, the result u."""
+    g = g * c
+    m2 = b1 * m + (1 - b1) * g
+    v2 = b2 * v + (1 - b2) * g * g
+    root = torch.sqrt(v2 / (1 - b2 ** t)) + eps
+    size = lr / (1 - b1 ** t)
+    w2 = w * (1 - lr * wd) - size * m2 / root
+    dm = U * ((b1 * m).abs() + 4 * ((1 - b1) * g).abs() + m2.abs())
+    dw = size / root * dm + 10 * U * (size * m2 / root).abs() + U * (2 * w.abs() + w2.abs())
+    least = 2.0 ** -140                    # denormals
+    return m2, v2, w2, dm * SMALL + least, 8 * U * v2 * SMALL + least, dw * SMALL + least
+
+
+@pytest.mark.parametrize("master", [True, False])
+@pytest.mark.parametrize("sizes,types,shift", [([1], ["f32"], 0), (EDGES, ["f32"], 0), (EDGES, ["f32"], 3), (EDGES, ["bf16"], 0),
+                                               (EDGES, ["bf16", "f32", "f16"], 0), (EDGES, ["f16", "f32", "bf16"], 1),
+                                               ([3_000_001, 77], ["bf16"], 0), ([17] * 300, ["bf16", "f32"], 0)])
+@pytest.mark.parametrize("per_tensor", [True, False])
+def test_adamw(sizes, types, shift, master, per_tensor):
+    if not master and types != ["f32"]:
+        pytest.skip("without master weights the tensors are fp32")
+    workers = T.make(sizes, types, 1, shift, seed=7, scale=0.1)
+    ctx, lst, norms, ws = setup(workers)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(8)
+    flat = lambda: torch.randn(lst.d, device="cuda", generator=gen)  # noqa: E731
+    grad, m, v = flat(), flat() * 0.1, flat().square() * 0.01
+    wm = flat() if master else None
+    lr, step = torch.full((1,), 1e-2, device="cuda"), torch.full((1,), 4, dtype=torch.int64, device="cuda")
+    decay = torch.arange(len(sizes), device="cuda").float() * 0.01 if per_tensor else None
+    b1, b2, eps = 0.9, 0.99, 1e-6
+    inside = torch.zeros(lst.d, dtype=torch.bool, device="cuda")
+    for x in lst.views(inside):
+        x.fill_(True)
+    for t in (5, 6, 7):
+        old = [x.clone() for x in (m, v)] + ([wm.clone()] if master else [])
+        weights = [x.double() for x in (lst.views(wm) if master else workers[0])]
+        before = [x.double() for x in (grad, m, v)]
+        most = 0.5 * T.norm(lst.views(grad)) if t < 7 else math.inf
+        ctx.adamw(grad, lst, lr, step, m, v, norms, ws, master=wm, decay=decay, betas=(b1, b2), eps=eps, weight_decay=0.05, max_norm=most)
+        assert int(step) == t
+        r, = check_norms(norms, [lst.views(grad)])
+        for i, x in enumerate(workers[0]):
+            g0, m0, v0 = (lst.views(y)[i] for y in before)
+            wd = float(decay[i]) if per_tensor else 0.05
+            m2, v2, w2, dm, dv, dw = adam_exact(g0, m0, v0, weights[i], T.factor(r, most), t, float(lr), wd, b1, b2, eps)
+            T.within(lst.views(m)[i], m2, dm)
+            T.within(lst.views(v)[i], v2, dv)
+            if master:
+                T.within(lst.views(wm)[i], w2, dw)
+                assert torch.equal(x, lst.views(wm)[i].to(x.dtype))
+            else:
+                T.within(x, w2, dw)
+        for y, o in zip([m, v] + ([wm] if master else []), old):
+            assert torch.equal(y[~inside], o[~inside])
+
+
+def test_adamw_skips_a_step_whose_norm_is_not_finite():
+    from paper_2302_08545_b200 import thc
+    workers = T.make([5000, 10], ["bf16"], 1)
+    ctx, lst, norms, ws = setup(workers)
+    grad = torch.randn(lst.d, device="cuda")
+    grad[lst.offsets[1] - 1] = math.nan    # between the tensors: does not matter
+    m, v, w = (torch.rand(lst.d, device="cuda") for _ in range(3))
+    lr, step = torch.full((1,), 1e-2, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    ctx.adamw(grad, lst, lr, step, m, v, norms, ws, master=w, max_norm=1.0)
+    assert int(step) == 1 and ctx.status() == 0
+    held = [x.clone() for x in (m, v, w, *workers[0])]
+    for bad in (math.nan, math.inf):
+        grad[5] = bad
+        ctx.adamw(grad, lst, lr, step, m, v, norms, ws, master=w, max_norm=1.0)
+        assert int(step) == 1 and ctx.status() == thc.STATUS_NONFINITE
+        assert all(torch.equal(x, y) for x, y in zip(held, (m, v, w, *workers[0])))
+
+
+def test_other_addresses():
+    """Gradients that are allocated anew: the list takes the new addresses from then on."""
+    sizes, types = [100, 3000, 1] * 200, ["f32", "bf16"]   # more addresses than one launch takes
+    first, second = T.make(sizes, types, 2, seed=1), T.make(sizes, types, 2, seed=2, shift=1)
+    ctx, lst, norms, ws = setup(first)
+    ctx.grad_norm(lst, norms, ws)
+    check_norms(norms, first)
+    lst.assign(second)
+    ctx.grad_norm(lst, norms, ws)
+    check_norms(norms, second)
+    with pytest.raises(ValueError):
+        lst.assign([first[0]])
+    with pytest.raises(ValueError):
+        lst.assign([[x.double() for x in w] for w in first])
+    ctx.grad_norm(lst, norms, ws)
+    check_norms(norms, second)
+
+
+def test_captured_and_replayed_on_another_stream():
+    workers = T.make([5000, 64, 100_001], ["bf16"], 1, seed=3)
+    ctx, lst, norms, ws = setup(workers)
+    grad = torch.randn(lst.d, device="cuda")
+    state = [torch.rand(lst.d, device="cuda") for _ in range(3)]
+    lr, step = torch.full((1,), 1e-2, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def call():
+        m, v, w = state
+        ctx.adamw(grad, lst, lr, step, m, v, norms, ws, master=w, max_norm=1.0)
+    held = [x.clone() for x in (*state, *workers[0])]
+    for k in range(3):
+        if k == 2:
+            lr.fill_(5e-3)
+        call()
+    torch.cuda.synchronize()
+    expected = [x.clone() for x in (*state, *workers[0])]
+    for x, y in zip((*state, *workers[0]), held):
+        x.copy_(y)
+    step.zero_()
+    lr.fill_(1e-2)
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for k in range(3):
+        if k == 2:
+            lr.fill_(5e-3)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert int(step) == 3
+    assert all(torch.equal(x, y) for x, y in zip((*state, *workers[0]), expected))
+
+
+def test_refused_arguments():
+    from paper_2302_08545_b200 import thc
+    workers = T.make([100, 300], ["f32"], 2)
+    ctx, lst, norms, ws = setup(workers)
+    one = thc.Tensors(ctx, workers[:1])
+    half = thc.Tensors(ctx, T.make([100, 300], ["bf16"], 1))
+    flat = lambda n=1: [torch.zeros(lst.d, device="cuda") for _ in range(n)]  # noqa: E731
+    f = flat(2)
+    lr, step = torch.ones(1, device="cuda"), torch.ones(1, dtype=torch.int64, device="cuda")
+    g, m, v, w = flat(4)
+    inf = math.inf
+
+    def code(call):
+        with pytest.raises(thc.ThcError) as e:
+            call()
+        return e.value.code
+    EINVAL = thc.THC_EINVAL
+    assert code(lambda: ctx.grad_norm(lst, norms, ws[:64])) == thc.THC_EWORKSPACE
+    assert code(lambda: ctx.grad_norm(lst, None, ws)) == EINVAL
+    assert code(lambda: ctx.grad_norm(lst, norms, None)) == EINVAL
+    assert code(lambda: ctx.clip_grads(lst, -1.0, norms, ws)) == EINVAL
+    assert code(lambda: ctx.clip_grads(lst, math.nan, norms, ws)) == EINVAL
+    assert code(lambda: ctx.clip_grads(one, 1.0, norms, ws, out=half)) == EINVAL
+    assert code(lambda: ctx.clip_grads(lst, 1.0, norms, ws, out=one)) == EINVAL
+    assert code(lambda: ctx.clip_grads(lst, 1.0, None, ws)) == EINVAL
+    # the same tensor twice, and an output that lies across an input
+    twice = thc.Tensors(ctx, [[workers[0][0], workers[0][0]]])
+    ctx.grad_norm(twice, norms, ws)
+    assert code(lambda: ctx.clip_grads(twice, 1.0, norms, ws)) == EINVAL
+    room = torch.zeros(1000, device="cuda")
+    a, b = thc.Tensors(ctx, [[room[:100], room[200:500]]]), thc.Tensors(ctx, [[room[8:108], room[600:900]]])
+    assert code(lambda: ctx.clip_grads(a, 1.0, norms, ws, out=b)) == EINVAL
+    same = thc.Tensors(ctx, [[room[:100], room[600:900]]])
+    ctx.clip_grads(a, 1.0, norms, ws, out=same)
+    assert code(lambda: ctx.gather_grads(lst, 1.0, f, None, None)) == EINVAL
+    assert code(lambda: ctx.gather_grads(lst, 1.0, [f[0], f[0]], norms, ws)) == EINVAL
+    assert code(lambda: ctx.gather_grads(lst, 1.0, f, norms, ws, ef=[f[1], f[0]])) == EINVAL
+    assert code(lambda: ctx.gather_grads(lst, 1.0, [f[0], None], norms, ws)) == EINVAL
+    assert code(lambda: ctx.gather_grads(thc.Tensors(ctx, [[f[0][:100], f[1][:300]]]), 1.0, f[:1], norms, ws)) == EINVAL
+    wide = context("bf16")
+    assert code(lambda: wide.gather_grads(thc.Tensors(wide, workers), 1.0, [x.bfloat16() for x in f], norms, ws, ef=f)) == thc.THC_EUNSUPPORTED
+    assert code(lambda: ctx.scatter_grads(f[0], 1.0, lst, norms, ws)) == EINVAL             # two workers
+    assert code(lambda: ctx.scatter_grads(f[0], 1.0, thc.Tensors(ctx, [[f[0][4:104], f[0][128:428]]]), norms, ws)) == EINVAL
+    step_ok = dict(betas=(0.9, 0.99), max_norm=inf)
+    assert code(lambda: ctx.adamw(g, half, lr, step, m, v, norms, ws, **step_ok)) == EINVAL  # no master weights
+    assert code(lambda: ctx.adamw(g, lst, lr, step, m, v, norms, ws, master=w, **step_ok)) == EINVAL
+    assert code(lambda: ctx.adamw(g, one, lr, step, m, m, norms, ws, **step_ok)) == EINVAL
+    assert code(lambda: ctx.adamw(g, one, lr, step, m, v, norms, ws, master=g, **step_ok)) == EINVAL
+    assert code(lambda: ctx.adamw(g, one, None, step, m, v, norms, ws, **step_ok)) == EINVAL
+    for bad in (dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(betas=(math.nan, 0.9)), dict(eps=-1.0), dict(eps=inf),
+                dict(weight_decay=-1.0), dict(weight_decay=math.nan), dict(max_norm=math.nan)):
+        assert code(lambda: ctx.adamw(g, one, lr, step, m, v, norms, ws, **dict(step_ok, **bad))) == EINVAL
+    # what the library cannot see from an address
+    for call in (lambda: ctx.grad_norm(lst, norms[:1], ws), lambda: ctx.grad_norm(lst, norms.double(), ws),
+                 lambda: ctx.grad_norm(lst, norms.cpu(), ws),
+                 lambda: ctx.gather_grads(lst, 1.0, [x[:-1] for x in f], norms, ws), lambda: ctx.gather_grads(lst, 1.0, f[:1], norms, ws),
+                 lambda: ctx.gather_grads(lst, 1.0, [x.bfloat16() for x in f], norms, ws),
+                 lambda: ctx.gather_grads(lst, 1.0, f, norms, ws, ef=[x[:-1] for x in f]),
+                 lambda: ctx.scatter_grads(torch.zeros(2 * lst.d, device="cuda")[::2], 1.0, one, norms, ws),
+                 lambda: ctx.adamw(g, one, lr, step.int(), m, v, norms, ws), lambda: ctx.adamw(g, one, lr, step, m[:-1], v, norms, ws),
+                 lambda: ctx.adamw(g, one, lr, step, m, v, norms, ws, decay=lr),
+                 lambda: thc.Tensors(ctx, [[room[::2]]]), lambda: thc.Tensors(ctx, [[room.double()]]), lambda: thc.Tensors(ctx, [[room.cpu()]]),
+                 lambda: thc.Tensors(ctx, [[room], [room[:-1]]]), lambda: thc.Tensors(ctx, [[room], [room, room]]), lambda: thc.Tensors(ctx, []),
+                 lambda: thc.Tensors(ctx, [[]])):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(thc.ThcError):
+        thc.Tensors(ctx, [[torch.zeros(0, device="cuda")]])
+    half.close()
+    with pytest.raises(ValueError):
+        ctx.clip_grads(one, 1.0, norms, ws, out=half)
+    assert code(lambda: ctx.grad_norm(half, norms, ws)) == EINVAL
+    torch.cuda.synchronize()
