@@ -734,7 +734,7 @@ static_assert(1024 + (4 << 13) + (1 << 13) / 4 + 1024 * 16 + 256 * kLutEntryByte
 // Lets a kernel use more than the default 48 KB.  The limit is the same for every launch of every kernel, so
 // that no thread can lower it between another's call and its launch; what is done is remembered per kernel
 // and device, and done again (to the same effect) should the table be full.
-static int ensure_dynamic_smem(const void *kern)
+int thc::ensure_dynamic_smem(const void *kern)
 {
     constexpr uint32_t kSlots = 2048;                  // of some 300 kernels
     static std::mutex guard;

@@ -28,6 +28,9 @@ CtxView view_of(const thc_ctx *ctx);
 // Whether the context can launch on the current device (THC_OK, THC_EINVAL, THC_ECUDA).
 int check_launch_ctx(const thc_ctx *ctx);
 
+// Lets a kernel use more than the default 48 KB of dynamic shared memory (up to 120 KB).
+int ensure_dynamic_smem(const void *kern);
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // A launch that may start while the one before it on the stream is still running (depend_on_previous):

@@ -7,9 +7,9 @@
 // names its flat position, from which every address follows (the table of tensor addresses holds the address that
 // flat position 0 would have).
 //
-// Clipping needs the norm of everything before the first product, so a call is two launches: the sums, whose last
-// CTA forms norm and factor, and the products, which go through the pieces backwards because what was
-// read last is still in L2.
+// Clipping needs the norm of everything before the first product.  One launch does both: sums of squares, a barrier
+// among the CTAs of a worker, products.  What a warp read last stays in shared memory (up to 8 KB a warp, 28 MB in all), the
+// rest is read again, backwards, because what was read last is still in L2.
 #include "thc_host.h"
 
 #include <algorithm>
@@ -25,7 +25,8 @@ namespace thc {
 constexpr uint32_t kPiece = 2048;              // elements of a piece: eight units of eight per lane
 constexpr uint32_t kUnit = 8;                  // consecutive elements of a lane: 16 bytes of a 16-bit type, 32 of fp32
 constexpr int kListThreads = 256, kListWarps = kListThreads / 32;
-constexpr uint32_t kNormCtasPerSm = 4, kMoveCtasPerSm = 4;
+constexpr uint32_t kNormCtasPerSm = 4, kClipCtasPerSm = 3;
+constexpr uint32_t kHeldBytes = 8192;          // per warp: a piece of fp32
 
 // {flat position (64 bits), tensor, length (16 bits) and type}
 struct Piece { uint64_t flat; uint32_t tensor, len_type; };
@@ -42,19 +43,11 @@ struct ListTable {
 struct Factor { float factor, scale; };
 __device__ __forceinline__ float times(const Factor &c, float x) { return c.factor * (x * c.scale); }
 
-// What the sums' last CTA leaves for the products.
-struct alignas(16) NormResult { Factor c; uint32_t skip, pad_; float step_size, inv_sqrt_by2, pad2_[2]; };
-
 struct NormOut {
     double *partial;             // [n][gridDim.x]
-    NormResult *result;          // [n]
     float *norms;                // or null
     DeviceBlock *dev;
     double max_norm;
-    // Adam step
-    const float *lr;             // null: none
-    int64_t *step;
-    double beta1, beta2;
 };
 
 __device__ __forceinline__ Piece load_piece(const Piece *p)
@@ -135,9 +128,36 @@ __device__ __forceinline__ void store_unit8(uint64_t a, const float (&v)[8])
 template <uint32_t T>
 __device__ __forceinline__ uint32_t head_of(uint64_t a) { return (uint32_t)((0ull - a) / size_of<T>()) & (kUnit - 1u); }
 
-// ---------------------------------------------------------------------------------- norm
+// ---------------------------------------------------------------------------------- held units
+// Units of the pieces that a warp read last, in its part of shared memory; a lane reads what it wrote itself.
+// 16 bytes of a lane next to its neighbours': no bank conflicts.
 template <uint32_t T>
-__device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uint32_t lane)
+__device__ __forceinline__ void hold_unit(uint32_t held, uint32_t b, uint32_t lane, const Raw<T> &r)
+{
+    constexpr uint32_t kParts = T == THC_F32 ? 2 : 1;
+#pragma unroll
+    for (uint32_t i = 0; i < kParts; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                     :: "r"(held + (b * kParts + i) * 512u + lane * 16u), "r"(r.w[4 * i]), "r"(r.w[4 * i + 1]), "r"(r.w[4 * i + 2]), "r"(r.w[4 * i + 3]) : "memory");
+}
+template <uint32_t T>
+__device__ __forceinline__ Raw<T> held_unit(uint32_t held, uint32_t b, uint32_t lane)
+{
+    constexpr uint32_t kParts = T == THC_F32 ? 2 : 1;
+    Raw<T> r;
+#pragma unroll
+    for (uint32_t i = 0; i < kParts; ++i)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r.w[4 * i]), "=r"(r.w[4 * i + 1]), "=r"(r.w[4 * i + 2]), "=r"(r.w[4 * i + 3])
+                     : "r"(held + (b * kParts + i) * 512u + lane * 16u));
+    return r;
+}
+constexpr uint32_t kNotHeld = 0xFFFFFFFFu;
+
+// ---------------------------------------------------------------------------------- norm
+// Sum of squares of a piece, in a lane; its units go to `held` unless that is kNotHeld.
+template <uint32_t T, bool HOLD>
+__device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uint32_t lane, uint32_t held)
 {
     constexpr int kBatch = T == THC_F32 ? 4 : 8;
     double s[2] = {0.0, 0.0};
@@ -147,16 +167,18 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
     float edge = 0.0f;
     if (lane < 8u ? single < head : lane < 16u && single < len) edge = load_one<T>(a + (uint64_t)single * size_of<T>());
     uint64_t at = a + head * size_of<T>();
+    uint32_t first = 0;                                // unit of the batch, in rows of 32
     // a whole batch, or what is left: lanes without a unit load the last one again and add nothing
     const auto batch = [&](auto whole, uint32_t left) {
+        constexpr bool kWhole = decltype(whole)::value;
         Raw<T> r[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b)
-            r[b] = load_unit8<T>(decltype(whole)::value ? at + 32u * b * kUnit * size_of<T>()
-                                                        : at + min(lane + 32u * b, left - 1u) * (kUnit * size_of<T>()));
+            r[b] = load_unit8<T>(at + (kWhole ? lane + 32u * b : min(lane + 32u * b, left - 1u)) * (kUnit * size_of<T>()));
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-            if (!decltype(whole)::value && lane + 32u * b >= left) r[b] = Raw<T>{};
+            if (HOLD && held != kNotHeld) hold_unit<T>(held, first + b, lane, r[b]);
+            if (!kWhole && lane + 32u * b >= left) r[b] = Raw<T>{};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const double v = (double)value<T>(r[b], e);
@@ -164,55 +186,48 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
             }
         }
         at += 32u * kBatch * kUnit * size_of<T>();
+        first += kBatch;
     };
     uint32_t u = 0;
 #pragma unroll 1
-    for (at += lane * (kUnit * size_of<T>()); u + 32u * kBatch <= units; u += 32u * kBatch) batch(std::true_type{}, 0u);
-    at -= lane * (kUnit * size_of<T>());
+    for (; u + 32u * kBatch <= units; u += 32u * kBatch) batch(std::true_type{}, 0u);
     if (u < units) batch(std::false_type{}, units - u);
     const double v = (double)edge;
     return fma(v, v, s[0]) + s[1];
 }
 
-__device__ __forceinline__ double squares(const ListTable &L, const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane)
+template <bool HOLD>
+__device__ __forceinline__ double squares(const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane, uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu, type = p.len_type >> 16;
-    if (flat != 0) return squares_of_piece<THC_F32>(flat + p.flat * 4u, len, lane);
+    if (flat != 0) return squares_of_piece<THC_F32, HOLD>(flat + p.flat * 4u, len, lane, held);
     const uint64_t b = load_base(base + p.tensor);
-    if (type == THC_F32) return squares_of_piece<THC_F32>(b + p.flat * 4u, len, lane);
-    if (type == THC_BF16) return squares_of_piece<THC_BF16>(b + p.flat * 2u, len, lane);
-    return squares_of_piece<THC_F16>(b + p.flat * 2u, len, lane);
+    if (type == THC_F32) return squares_of_piece<THC_F32, HOLD>(b + p.flat * 4u, len, lane, held);
+    if (type == THC_BF16) return squares_of_piece<THC_BF16, HOLD>(b + p.flat * 2u, len, lane, held);
+    return squares_of_piece<THC_F16, HOLD>(b + p.flat * 2u, len, lane, held);
 }
 
-// Norm, factor and what the Adam step needs, from a worker's sum of squares.
-__device__ __forceinline__ void finish_norm(const NormOut &o, uint32_t worker, double sum)
+// Sum over the CTA's threads, in thread 0.
+__device__ __forceinline__ double sum_of_cta(double s, double (&red)[kListWarps])
 {
-    const double norm = sqrt(sum);
-    NormResult r{};
-    r.c = Factor{1.0f, 1.0f};
-    if (!isinf(o.max_norm)) {
-        const double c = o.max_norm / (norm + 1e-6);
-        if (c < 0x1p-126) r.c = Factor{(float)(c * 0x1p126), 0x1p-126f};
-        else r.c.factor = c > 1.0 ? 1.0f : (float)c;   // NaN stays
-    }
-    const bool finite = isfinite(norm);
-    if (!finite) atomicOr(&o.dev->status, THC_STATUS_NONFINITE);
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, off);
+    if ((threadIdx.x & 31u) == 0) red[threadIdx.x >> 5] = s;
+    __syncthreads();
+    double t = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kListWarps; ++w) t += red[w];
+    return t;
+}
+
+__device__ __forceinline__ void report_norm(const NormOut &o, uint32_t worker, double norm)
+{
+    if (!isfinite(norm)) atomicOr(&o.dev->status, THC_STATUS_NONFINITE);
     if (o.norms != nullptr) o.norms[worker] = (float)norm;
-    if (o.lr != nullptr) {
-        r.skip = finite ? 0u : 1u;
-        if (finite) {
-            const int64_t t = *o.step + 1;
-            *o.step = t;
-            r.step_size = (float)((double)*o.lr / (1.0 - pow(o.beta1, (double)t)));
-            r.inv_sqrt_by2 = (float)(1.0 / sqrt(1.0 - pow(o.beta2, (double)t)));
-        }
-    }
-    o.result[worker] = r;
 }
 
 // Sums of squares of all pieces; a warp's pieces are fixed by the grid and the sums are added in a fixed order.
 __global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
-list_norm_kernel(const __grid_constant__ ListTable L, const __grid_constant__ NormOut o, uint64_t flat)
+list_norm_kernel(const __grid_constant__ ListTable L, const __grid_constant__ NormOut o)
 {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
     const uint32_t stride = gridDim.x * kListWarps;
@@ -227,16 +242,12 @@ list_norm_kernel(const __grid_constant__ ListTable L, const __grid_constant__ No
         const Piece now = p;
         c += stride;
         if (c < L.pieces_n) p = load_piece(L.pieces + c);
-        s += squares(L, now, base, flat, lane);
+        s += squares<false>(now, base, 0, lane, kNotHeld);
     }
     __shared__ double red[kListWarps];
     __shared__ uint32_t last;
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, off);
-    if (lane == 0) red[warp] = s;
-    __syncthreads();
+    double t = sum_of_cta(s, red);
     if (threadIdx.x == 0) {
-        double t = 0.0;
-        for (int w = 0; w < kListWarps; ++w) t += red[w];
         __stcg(o.partial + (uint64_t)worker * gridDim.x + blockIdx.x, t);
         __threadfence();
         last = atomicInc(o.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
@@ -244,22 +255,16 @@ list_norm_kernel(const __grid_constant__ ListTable L, const __grid_constant__ No
     __syncthreads();
     if (!last) return;
     __threadfence();
-    double t = 0.0;
+    t = 0.0;
     for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) t += __ldcg(o.partial + (uint64_t)worker * gridDim.x + i);
-    for (int off = 16; off > 0; off >>= 1) t += __shfl_down_sync(0xFFFFFFFFu, t, off);
-    if (lane == 0) red[warp] = t;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        t = 0.0;
-        for (int w = 0; w < kListWarps; ++w) t += red[w];
-        finish_norm(o, worker, t);
-    }
+    t = sum_of_cta(t, red);
+    if (threadIdx.x == 0) report_norm(o, worker, sqrt(t));
 }
 
 // ---------------------------------------------------------------------------------- products
-// y = c x (+ e) for a piece; zeros (or e) from its end up to dst_len.
+// y = c x (+ e) for a piece, whose units are in `held` unless that is kNotHeld; zeros (or e) from its end up to dst_len.
 template <uint32_t S, uint32_t D, bool EF>
-__device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t ef, uint32_t len, uint32_t dst_len, const Factor &c, uint32_t lane)
+__device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t ef, uint32_t len, uint32_t dst_len, const Factor &c, uint32_t lane, uint32_t held)
 {
     const auto product = [&c](float x, float e) { return EF ? fmaf(c.factor, x * c.scale, e) : times(c, x); };
     const uint32_t h = min(head_of<S>(src), len);
@@ -267,6 +272,7 @@ __device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t 
         constexpr int kBatch = EF ? 2 : S == THC_F32 ? 4 : 8;
         const uint32_t units = (len - h) / kUnit;
         uint64_t s = src + h * size_of<S>(), d = dst + h * size_of<D>(), q = ef + h * 4u;
+        uint32_t first = 0;
         // a whole batch, or what is left: lanes without a unit load the last one again and store nothing
         const auto batch = [&](auto whole, uint32_t left) {
             constexpr bool kWhole = decltype(whole)::value;
@@ -275,9 +281,10 @@ __device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t 
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 const uint32_t v = (kWhole ? lane + 32u * b : min(lane + 32u * b, left - 1u)) * kUnit;
-                x[b] = load_unit8<S>(s + v * size_of<S>());
+                x[b] = held != kNotHeld ? held_unit<S>(held, first + b, lane) : load_unit8<S>(s + v * size_of<S>());
                 if constexpr (EF) r[b] = load_unit8<THC_F32>(q + v * 4u);
             }
+            first += kBatch;
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 if (!kWhole && lane + 32u * b >= left) break;
@@ -330,71 +337,13 @@ __device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t 
         store_one<D>(dst + j * size_of<D>(), EF ? load_one<THC_F32>(ef + j * 4u) : 0.0f);
 }
 
-enum MoveKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter };
-
-struct MoveParams {
-    ListTable src, dst;          // kClip; kGather*: src; kScatter: dst
-    const NormResult *result;    // null: factor 1
-    uint64_t src_flat;           // kScatter
-    uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS];   // kGather*
-};
-
-template <MoveKind K, uint32_t T>
-__device__ __forceinline__ void move_typed(const MoveParams &P, const Piece &p, uint32_t worker, const Factor &c, uint32_t lane)
-{
-    const uint32_t len = p.len_type & 0xFFFFu;
-    const uint64_t at = p.flat * size_of<T>();
-    if (K == kClip) {
-        const uint64_t i = (uint64_t)worker * P.src.count + p.tensor;
-        move_piece<T, T, false>(load_base(P.src.base + i) + at, load_base(P.dst.base + i) + at, 0, len, len, c, lane);
-    } else if (K == kScatter) {
-        move_piece<THC_F32, T, false>(P.src_flat + p.flat * 4u, load_base(P.dst.base + p.tensor) + at, 0, len, len, c, lane);
-    } else {
-        constexpr uint32_t D = K == kGatherBf16 ? THC_BF16 : THC_F32;
-        const uint64_t src = load_base(P.src.base + (uint64_t)worker * P.src.count + p.tensor) + at;
-        const uint32_t full = (len + THC_TENSOR_ALIGN - 1u) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
-        move_piece<T, D, K == kGatherResidual>(src, P.dst_flat[worker] + p.flat * size_of<D>(),
-                                               K == kGatherResidual ? P.ef[worker] + p.flat * 4u : 0, len, full, c, lane);
-    }
-}
-
-template <MoveKind K>
-__global__ void __launch_bounds__(kListThreads, kMoveCtasPerSm)
-list_move_kernel(const __grid_constant__ MoveParams P)
-{
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
-    const ListTable &L = K == kScatter ? P.dst : P.src;
-    const uint32_t stride = gridDim.x * kListWarps;
-    uint32_t c = blockIdx.x * kListWarps + warp;
-    Piece p{};
-    if (c < L.pieces_n) p = load_piece(L.pieces + (L.pieces_n - 1u - c));
-    depend_on_previous();
-    Factor factor{1.0f, 1.0f};
-    if (P.result != nullptr) {
-        const uint2 q = ld_global(reinterpret_cast<const uint2 *>(&P.result[worker].c));
-        factor = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
-    }
-#pragma unroll 1
-    while (c < L.pieces_n) {
-        const Piece now = p;
-        c += stride;
-        if (c < L.pieces_n) p = load_piece(L.pieces + (L.pieces_n - 1u - c));
-        const uint32_t type = now.len_type >> 16;
-        if (type == THC_F32) move_typed<K, THC_F32>(P, now, worker, factor, lane);
-        else if (type == THC_BF16) move_typed<K, THC_BF16>(P, now, worker, factor, lane);
-        else move_typed<K, THC_F16>(P, now, worker, factor, lane);
-    }
-}
-
 // ---------------------------------------------------------------------------------- Adam
 struct AdamParams {
-    ListTable L;
-    const NormResult *result;
     const float *grad;
     float *master, *m, *v;       // master null: the tensors are the weights
     const float *lr, *decay;     // decay null: weight_decay
-    float beta1, beta2, one_less_beta1, one_less_beta2, eps;
-    double weight_decay;
+    int64_t *step;
+    double beta1, beta2, eps, weight_decay;
 };
 
 struct AdamStep { Factor c; float b1, b2, a1, a2, eps, step_size, inv_sqrt_by2, keep; };
@@ -410,22 +359,29 @@ __device__ __forceinline__ float adam(const AdamStep &k, float g, float &m, floa
 }
 
 template <uint32_t T, bool MASTER>
-__device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &k, const Piece &p, uint32_t lane)
+__device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &k, const Piece &p, uint64_t tensor, uint32_t lane, uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu;
     const uint64_t at = p.flat * 4u;
     const uint64_t g = reinterpret_cast<uint64_t>(P.grad) + at, m = reinterpret_cast<uint64_t>(P.m) + at,
-                   v = reinterpret_cast<uint64_t>(P.v) + at, out = load_base(P.L.base + p.tensor) + p.flat * size_of<T>();
+                   v = reinterpret_cast<uint64_t>(P.v) + at, out = tensor + p.flat * size_of<T>();
     const uint64_t w = MASTER ? reinterpret_cast<uint64_t>(P.master) + at : out;
     uint32_t done = 0;
-    if (((g | m | v | w) & 31u) == 0 && head_of<T>(out) == 0u) {
+    if (((g | m | v) & 31u) == 0 && (!MASTER || (w & 31u) == 0)) {
+        const bool whole = head_of<T>(out) == 0u;      // the tensor too takes units, else elements
         const uint32_t units = len / kUnit;
         done = units * kUnit;
+        uint32_t row = 0;
 #pragma unroll 1
-        for (uint32_t u = lane; u < units; u += 32u) {
-            const uint64_t o = (uint64_t)u * (kUnit * 4u);
-            const Raw<THC_F32> rg = load_unit8<THC_F32>(g + o), rm = load_unit8<THC_F32>(m + o), rv = load_unit8<THC_F32>(v + o),
-                               rw = load_unit8<THC_F32>(w + o);
+        for (uint32_t u = lane; u < units; u += 32u, ++row) {
+            const uint64_t o = (uint64_t)u * (kUnit * 4u), to = out + (uint64_t)u * (kUnit * size_of<T>());
+            const Raw<THC_F32> rm = load_unit8<THC_F32>(m + o), rv = load_unit8<THC_F32>(v + o);
+            Raw<THC_F32> rw;
+            if (MASTER || whole) rw = load_unit8<THC_F32>(w + o);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) rw.w[e] = ld_global(reinterpret_cast<const uint32_t *>(w + o + 4u * e));
+            const Raw<THC_F32> rg = held != kNotHeld ? held_unit<THC_F32>(held, row, lane) : load_unit8<THC_F32>(g + o);
             float ym[8], yv[8], yw[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -436,7 +392,10 @@ __device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &
             store_unit8<THC_F32>(m + o, ym);
             store_unit8<THC_F32>(v + o, yv);
             if (MASTER) store_unit8<THC_F32>(w + o, yw);
-            store_unit8<T>(out + (uint64_t)u * (kUnit * size_of<T>()), yw);
+            if (whole) store_unit8<T>(to, yw);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) store_one<T>(to + size_of<T>() * e, yw[e]);
         }
     }
     for (uint32_t j = done + lane; j < len; j += 32u) {
@@ -450,33 +409,176 @@ __device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &
     }
 }
 
-template <bool MASTER>
-__global__ void __launch_bounds__(kListThreads, 2)
-list_adam_kernel(const __grid_constant__ AdamParams P)
+// ---------------------------------------------------------------------------------- the calls that clip
+enum ClipKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter, kAdam, kAdamMaster };
+
+struct ClipParams {
+    ListTable L;                 // whose pieces are walked
+    const uint64_t *dst_base;    // kClip: addresses of the tensors that are written
+    NormOut o;
+    uint32_t with_norm;          // 0: no norm, factor 1
+    uint32_t split_log2;         // a warp takes a 2^-split_log2 of a piece at a time
+    uint64_t src_flat;           // kScatter, kAdam*: what is read (else the tensors of L)
+    uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS];   // kGather*
+    AdamParams adam;
+};
+
+// Part `item` of all parts of the pieces; length 0 where a piece is too short to have it.
+__device__ __forceinline__ Piece load_item(const ListTable &L, uint32_t item, uint32_t split_log2)
 {
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint32_t stride = gridDim.x * kListWarps;
-    uint32_t c = blockIdx.x * kListWarps + warp;
-    Piece p{};
-    if (c < P.L.pieces_n) p = load_piece(P.L.pieces + (P.L.pieces_n - 1u - c));
+    Piece p = load_piece(L.pieces + (item >> split_log2));
+    const uint32_t part = kPiece >> split_log2, from = (item & ((1u << split_log2) - 1u)) * part, len = p.len_type & 0xFFFFu;
+    p.flat += from;
+    p.len_type = (p.len_type & 0xFFFF0000u) | (len > from ? min(len - from, part) : 0u);
+    return p;
+}
+
+template <ClipKind K, uint32_t T>
+__device__ __forceinline__ void move_typed(const ClipParams &P, const Piece &p, uint32_t worker, const Factor &c, uint32_t lane, uint32_t held)
+{
+    const uint32_t len = p.len_type & 0xFFFFu;
+    const uint64_t i = (uint64_t)worker * P.L.count + p.tensor, at = p.flat * size_of<T>(), tensor = load_base(P.L.base + i) + at;
+    if (K == kClip) {
+        move_piece<T, T, false>(tensor, load_base(P.dst_base + i) + at, 0, len, len, c, lane, held);
+    } else if (K == kScatter) {
+        move_piece<THC_F32, T, false>(P.src_flat + p.flat * 4u, tensor, 0, len, len, c, lane, held);
+    } else {
+        constexpr uint32_t D = K == kGatherBf16 ? THC_BF16 : THC_F32;
+        const uint32_t full = (len + THC_TENSOR_ALIGN - 1u) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
+        move_piece<T, D, K == kGatherResidual>(tensor, P.dst_flat[worker] + p.flat * size_of<D>(),
+                                               K == kGatherResidual ? P.ef[worker] + p.flat * 4u : 0, len, full, c, lane, held);
+    }
+}
+
+// Waits until all CTAs of the worker have added themselves to `arrived`; false if that takes some seconds (it cannot: the
+// launch is cooperative, so all of them run).
+__device__ __forceinline__ bool wait_for(const uint32_t *arrived, uint32_t ctas)
+{
+    for (uint32_t i = 0; i < (1u << 23); ++i) {
+        uint32_t v;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+        if (v >= ctas) return true;
+    }
+    return false;
+}
+
+// grid (CTAs of a worker, workers).  Phase 1: squares of the worker's pieces; the sums meet in the workspace, every CTA adds
+// all of them in the same order and forms norm and factor itself (one that did it for all would cost the others two
+// more trips to L2).  Phase 2: the products, the held pieces first.
+template <ClipKind K>
+__global__ void __launch_bounds__(kListThreads, kClipCtasPerSm)
+list_clip_kernel(const __grid_constant__ ClipParams P)
+{
+    constexpr bool kIsAdam = K == kAdam || K == kAdamMaster;
+    extern __shared__ __align__(16) unsigned char held_bytes[];
+    __shared__ double red[kListWarps];
+    __shared__ AdamStep s_step;
+    __shared__ uint32_t s_go;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(held_bytes) + warp * kHeldBytes;
+    const uint32_t stride = gridDim.x * kListWarps, items = P.L.pieces_n << P.split_log2;
+    const uint32_t first = blockIdx.x * kListWarps + warp;
+    const uint32_t mine = first < items ? (items - first + stride - 1u) / stride : 0u;
+    uint32_t in_slot = 0;                              // items of the warp that are held: its last one, or two of 16 bits
     depend_on_previous();
-    const uint4 q = ld_global(reinterpret_cast<const uint4 *>(P.result));
-    const uint2 sizes = ld_global(reinterpret_cast<const uint2 *>(&P.result->step_size));
-    if (q.z != 0u) return;                             // the norm is not finite
-    const float lr = ld_global(P.lr);
-    AdamStep k{Factor{__uint_as_float(q.x), __uint_as_float(q.y)}, P.beta1, P.beta2, P.one_less_beta1, P.one_less_beta2, P.eps,
-               __uint_as_float(sizes.x), __uint_as_float(sizes.y), 0.0f};
+    AdamStep k{};
+    k.c = Factor{1.0f, 1.0f};
+    float lr = 0.0f;
+    if (kIsAdam) lr = ld_global(P.adam.lr);
+    if (P.with_norm != 0u) {
+        const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
+        constexpr bool kFlat = kIsAdam || K == kScatter;
+        double s = 0.0;
+        Piece p{};
+        if (mine != 0u) p = load_item(P.L, first, P.split_log2);
 #pragma unroll 1
-    while (c < P.L.pieces_n) {
+        for (uint32_t i = 0; i < mine; ++i) {
+            const Piece now = p;
+            if (i + 1u < mine) p = load_item(P.L, first + (i + 1u) * stride, P.split_log2);
+            uint32_t held = kNotHeld;
+            if (i + 1u == mine) {
+                held = slot;                           // over the one before it unless both are of 16 bits
+                in_slot = in_slot != 0u && (now.len_type >> 16) != THC_F32 ? 2u : 1u;
+            } else if (!kFlat && i + 2u == mine && (now.len_type >> 16) != THC_F32) {
+                held = slot + kHeldBytes / 2;
+                in_slot = 1u;
+            }
+            s += squares<true>(now, base, kFlat ? P.src_flat : 0, lane, held);
+        }
+        // what the Adam step needs of its count, before the wait
+        double step_size = 0.0, by2 = 0.0;
+        int64_t t = 0;
+        if (kIsAdam && threadIdx.x == 0) {
+            t = (int64_t)load_base(reinterpret_cast<const uint64_t *>(P.adam.step)) + 1;
+            step_size = (double)lr / (1.0 - pow(P.adam.beta1, (double)t));
+            by2 = 1.0 / sqrt(1.0 - pow(P.adam.beta2, (double)t));
+        }
+        double sum = sum_of_cta(s, red);
+        uint32_t *arrived = P.o.dev->clip_arrived + worker, *left = P.o.dev->norm_counters + worker;
+        const double *partial = P.o.partial + (uint64_t)worker * gridDim.x;
+        if (threadIdx.x == 0) {
+            __stcg(P.o.partial + (uint64_t)worker * gridDim.x + blockIdx.x, sum);
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" :: "l"(arrived) : "memory");
+            s_go = wait_for(arrived, gridDim.x) ? 1u : 0u;
+            // the last one to leave clears the counter for the next launch
+            if (atomicInc(left, gridDim.x - 1u) == gridDim.x - 1u) atomicExch(arrived, 0u);
+        }
+        __syncthreads();
+        if (s_go == 0u) {
+            if (threadIdx.x == 0) atomicOr(&P.o.dev->status, THC_STATUS_WAIT_TIMEOUT);
+            return;
+        }
+        sum = 0.0;
+        for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(partial + i);
+        sum = sum_of_cta(sum, red);
+        if (threadIdx.x == 0) {
+            const double norm = sqrt(sum);
+            if (blockIdx.x == 0) report_norm(P.o, worker, norm);
+            Factor c{1.0f, 1.0f};
+            if (!isinf(P.o.max_norm)) {
+                const double f = P.o.max_norm / (norm + 1e-6);
+                if (f < 0x1p-126) c = Factor{(float)(f * 0x1p126), 0x1p-126f};
+                else c.factor = f > 1.0 ? 1.0f : (float)f;   // NaN stays
+            }
+            s_step.c = c;
+            if (kIsAdam) {
+                if (!isfinite(norm)) s_go = 0u;        // no step
+                else if (blockIdx.x == 0) *P.adam.step = t;
+                s_step.step_size = (float)step_size;
+                s_step.inv_sqrt_by2 = (float)by2;
+            }
+        }
+        __syncthreads();
+        if (s_go == 0u) return;
+        k = s_step;
+    }
+    if (kIsAdam) {
+        k.b1 = (float)P.adam.beta1;
+        k.b2 = (float)P.adam.beta2;
+        k.a1 = (float)(1.0 - P.adam.beta1);
+        k.a2 = (float)(1.0 - P.adam.beta2);
+        k.eps = (float)P.adam.eps;
+    }
+    Piece p{};
+    if (mine != 0u) p = load_item(P.L, first + (mine - 1u) * stride, P.split_log2);
+#pragma unroll 1
+    for (uint32_t i = mine; i-- > 0u;) {
         const Piece now = p;
-        c += stride;
-        if (c < P.L.pieces_n) p = load_piece(P.L.pieces + (P.L.pieces_n - 1u - c));
-        const double wd = P.decay != nullptr ? (double)ld_global(P.decay + now.tensor) : P.weight_decay;
-        k.keep = (float)(1.0 - (double)lr * wd);
+        if (i > 0u) p = load_item(P.L, first + (i - 1u) * stride, P.split_log2);
+        const uint32_t back = mine - 1u - i, held = back < in_slot ? slot + back * (kHeldBytes / 2) : kNotHeld;
         const uint32_t type = now.len_type >> 16;
-        if (!MASTER || type == THC_F32) adam_piece<THC_F32, MASTER>(P, k, now, lane);
-        else if (type == THC_BF16) adam_piece<THC_BF16, MASTER>(P, k, now, lane);
-        else adam_piece<THC_F16, MASTER>(P, k, now, lane);
+        if constexpr (kIsAdam) {
+            const double wd = P.adam.decay != nullptr ? (double)ld_global(P.adam.decay + now.tensor) : P.adam.weight_decay;
+            k.keep = (float)(1.0 - (double)lr * wd);
+            const uint64_t tensor = load_base(P.L.base + now.tensor);
+            if (K == kAdam || type == THC_F32) adam_piece<THC_F32, K == kAdamMaster>(P.adam, k, now, tensor, lane, held);
+            else if (type == THC_BF16) adam_piece<THC_BF16, K == kAdamMaster>(P.adam, k, now, tensor, lane, held);
+            else adam_piece<THC_F16, K == kAdamMaster>(P.adam, k, now, tensor, lane, held);
+        } else {
+            if (type == THC_F32) move_typed<K, THC_F32>(P, now, worker, k.c, lane, held);
+            else if (type == THC_BF16) move_typed<K, THC_BF16>(P, now, worker, k.c, lane, held);
+            else move_typed<K, THC_F16>(P, now, worker, k.c, lane, held);
+        }
     }
 }
 
@@ -629,19 +731,19 @@ int thc_tensors_destroy(thc_tensors *h)
     return THC_OK;
 }
 
-// CTAs per worker of a launch over all pieces.
-static uint32_t ctas_of(const thc_tensors *h, uint32_t per_sm)
+// CTAs per worker of a launch over all pieces, each cut into 2^split_log2 parts.
+static uint32_t ctas_of(const thc_tensors *h, uint32_t per_sm, uint32_t split_log2 = 0)
 {
     const uint32_t most = std::max(1u, h->sm_count * per_sm / h->n);
-    return std::min(most, (h->pieces_n + kListWarps - 1) / kListWarps);
+    return (uint32_t)std::min<uint64_t>(most, (((uint64_t)h->pieces_n << split_log2) + kListWarps - 1) / kListWarps);
 }
 
 static uint64_t round_up256(uint64_t v) { return (v + 255) / 256 * 256; }
 
-// Workspace: results of the workers, then the partial sums.
+// Workspace: the partial sums.
 static uint64_t workspace_need(const thc_tensors *h)
 {
-    return round_up256(h->n * sizeof(NormResult)) + round_up256((uint64_t)h->n * ctas_of(h, kNormCtasPerSm) * sizeof(double));
+    return round_up256((uint64_t)h->n * std::max(1u, h->sm_count * std::max(kNormCtasPerSm, kClipCtasPerSm) / h->n) * sizeof(double));
 }
 
 int thc_tensors_sizes(const thc_tensors *h, thc_tensors_sizes_t *s)
@@ -724,23 +826,15 @@ static bool overlaps(const thc_tensors *h, uint64_t lo, uint64_t hi)
     return it != h->ranges.end() && it->lo < hi;
 }
 
-static NormOut norm_out(const CtxView &v, const thc_tensors *h, double max_norm, float *norms, void *workspace)
+static NormOut norm_out(const CtxView &v, double max_norm, float *norms, void *workspace)
 {
     NormOut o;
     memset(&o, 0, sizeof o);
-    o.result = static_cast<NormResult *>(workspace);
-    o.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + round_up256(h->n * sizeof(NormResult)));
+    o.partial = static_cast<double *>(workspace);
     o.norms = norms;
     o.dev = v.dev;
     o.max_norm = max_norm;
     return o;
-}
-
-static int launch_norm(const thc_tensors *h, const NormOut &o, const void *flat, cudaStream_t st)
-{
-    THC_CUDA(launch_after(list_norm_kernel, dim3(ctas_of(h, kNormCtasPerSm), h->n), kListThreads, 0, st, table_of(h), o,
-                          reinterpret_cast<uint64_t>(flat)));
-    return THC_OK;
 }
 
 int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes, void *stream)
@@ -749,21 +843,41 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
     if (rc != THC_OK) return rc;
     if (norms == nullptr || !aligned4(norms)) return THC_EINVAL;
     if ((rc = check_workspace(list, workspace, workspace_bytes)) != THC_OK) return rc;
-    return launch_norm(list, norm_out(view_of(ctx), list, INFINITY, norms, workspace), nullptr, static_cast<cudaStream_t>(stream));
+    THC_CUDA(launch_after(list_norm_kernel, dim3(ctas_of(list, kNormCtasPerSm), list->n), kListThreads, 0, static_cast<cudaStream_t>(stream),
+                          table_of(list), norm_out(view_of(ctx), INFINITY, norms, workspace)));
+    return THC_OK;
 }
 
-// Norm (unless there is nothing to form from it), then the products.
-static int launch_move(thc_ctx *ctx, void (*kern)(MoveParams), MoveParams &P, const thc_tensors *h, const void *flat, double max_norm,
-                       float *norms, void *workspace, cudaStream_t st)
+// One launch of list_clip_kernel; cooperative where its CTAs wait for one another.
+static int launch_clip(thc_ctx *ctx, void (*kern)(ClipParams), ClipParams &P, const thc_tensors *h, double max_norm, float *norms,
+                       void *workspace, cudaStream_t st)
 {
-    P.result = nullptr;
-    if (norms != nullptr) {
-        const NormOut o = norm_out(view_of(ctx), h, max_norm, norms, workspace);
-        const int rc = launch_norm(h, o, flat, st);
-        if (rc != THC_OK) return rc;
-        P.result = o.result;
+    P.L = table_of(h);
+    P.with_norm = norms != nullptr ? 1u : 0u;
+    P.o = norm_out(view_of(ctx), max_norm, norms, workspace);
+    // A piece is eight units a lane, one after the other or four at a time: few pieces are cut so that more warps share them.
+    P.split_log2 = 0;
+    while (P.split_log2 < 3 && ((uint64_t)h->pieces_n * h->n << (P.split_log2 + 1)) <= (uint64_t)h->sm_count * kClipCtasPerSm * kListWarps) ++P.split_log2;
+    const uint32_t smem = kHeldBytes * kListWarps;
+    const int rc = ensure_dynamic_smem(reinterpret_cast<const void *>(kern));
+    if (rc != THC_OK) return rc;
+    cudaLaunchAttribute attr;
+    if (P.with_norm) {
+        attr.id = cudaLaunchAttributeCooperative;
+        attr.val.cooperative = 1;
+    } else {
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
     }
-    THC_CUDA(launch_after(kern, dim3(ctas_of(h, kMoveCtasPerSm), h->n), kListThreads, 0, st, P));
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(ctas_of(h, kClipCtasPerSm, P.split_log2), h->n);
+    cfg.blockDim = dim3(kListThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    THC_CUDA(cudaLaunchKernelEx(&cfg, kern, P));
     return THC_OK;
 }
 
@@ -793,11 +907,10 @@ int thc_clip_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const
             if (overlaps(out, r.lo, r.hi)) return THC_EINVAL;
         }
     }
-    MoveParams P;
+    ClipParams P;
     memset(&P, 0, sizeof P);
-    P.src = table_of(list);
-    P.dst = table_of(out);
-    return launch_move(ctx, list_move_kernel<kClip>, P, list, nullptr, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+    P.dst_base = out->base;
+    return launch_clip(ctx, list_clip_kernel<kClip>, P, list, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *const *ef_or_null, void *const *flats,
@@ -810,7 +923,7 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
     if (bf16 && ef_or_null != nullptr) return THC_EUNSUPPORTED;
     if (flats == nullptr) return THC_EINVAL;
     const uint64_t bytes = list->d * (bf16 ? 2u : 4u);
-    MoveParams P;
+    ClipParams P;
     memset(&P, 0, sizeof P);
     for (uint32_t i = 0; i < list->n; ++i) {
         if (flats[i] == nullptr || !aligned16(flats[i])) return THC_EINVAL;
@@ -828,9 +941,8 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
             if (ef_or_null != nullptr && !(j == i && P.ef[j] == P.dst_flat[i]) && !apart(P.dst_flat[i], P.ef[j])) return THC_EINVAL;
         }
     }
-    P.src = table_of(list);
-    return launch_move(ctx, ef_or_null != nullptr ? list_move_kernel<kGatherResidual> : bf16 ? list_move_kernel<kGatherBf16> : list_move_kernel<kGatherF32>,
-                       P, list, nullptr, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+    return launch_clip(ctx, ef_or_null != nullptr ? list_clip_kernel<kGatherResidual> : bf16 ? list_clip_kernel<kGatherBf16> : list_clip_kernel<kGatherF32>,
+                       P, list, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const thc_tensors *list, float *norms, void *workspace,
@@ -843,11 +955,10 @@ int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const th
     const uint64_t lo = reinterpret_cast<uint64_t>(flat), hi = lo + list->d * 4u;
     for (const auto &r : list->ranges)
         if (r.lo < hi && lo < r.hi && !(list->dtype[r.index] == THC_F32 && r.lo == lo + list->offset[r.index] * 4u)) return THC_EINVAL;
-    MoveParams P;
+    ClipParams P;
     memset(&P, 0, sizeof P);
-    P.dst = table_of(list);
     P.src_flat = lo;
-    return launch_move(ctx, list_move_kernel<kScatter>, P, list, flat, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+    return launch_clip(ctx, list_clip_kernel<kScatter>, P, list, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int thc_adamw(thc_ctx *ctx, const thc_adamw_config *cfg, const float *grad, const thc_tensors *list, const float *lr, int64_t *step,
@@ -874,31 +985,10 @@ int thc_adamw(thc_ctx *ctx, const thc_adamw_config *cfg, const float *grad, cons
             if (a < b + bytes && b < a + bytes) return THC_EINVAL;
         }
     }
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    NormOut o = norm_out(view_of(ctx), list, cfg->max_norm, norms, workspace);
-    o.lr = lr;
-    o.step = step;
-    o.beta1 = cfg->beta1;
-    o.beta2 = cfg->beta2;
-    if ((rc = launch_norm(list, o, grad, st)) != THC_OK) return rc;
-    AdamParams P;
+    ClipParams P;
     memset(&P, 0, sizeof P);
-    P.L = table_of(list);
-    P.result = o.result;
-    P.grad = grad;
-    P.master = master_or_null;
-    P.m = m;
-    P.v = v;
-    P.lr = lr;
-    P.decay = decay_or_null;
-    P.beta1 = (float)cfg->beta1;
-    P.beta2 = (float)cfg->beta2;
-    P.one_less_beta1 = (float)(1.0 - cfg->beta1);
-    P.one_less_beta2 = (float)(1.0 - cfg->beta2);
-    P.eps = (float)cfg->eps;
-    P.weight_decay = cfg->weight_decay;
-    const dim3 grid(ctas_of(list, 2));
-    if (master_or_null != nullptr) THC_CUDA(launch_after(list_adam_kernel<true>, grid, kListThreads, 0, st, P));
-    else THC_CUDA(launch_after(list_adam_kernel<false>, grid, kListThreads, 0, st, P));
-    return THC_OK;
+    P.src_flat = reinterpret_cast<uint64_t>(grad);
+    P.adam = AdamParams{grad, master_or_null, m, v, lr, decay_or_null, step, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay};
+    return launch_clip(ctx, master_or_null != nullptr ? list_clip_kernel<kAdamMaster> : list_clip_kernel<kAdam>, P, list, cfg->max_norm, norms,
+                       workspace, static_cast<cudaStream_t>(stream));
 }
