@@ -30,8 +30,7 @@ struct DeviceBlock {
     uint32_t range_keys[2 * kPrepCounters];    // exact range, up to as many blocks (self-resetting)
     uint4    lut[256];           // by floor(u*g): (-T[z0] as float, 65536/(T[z0+1]-T[z0]), z0, 0)
     uint32_t table[256];         // T
-    uint32_t norm_counters[THC_MAX_WORKERS];   // lists of tensors, per worker: CTAs that are done (self-resetting)
-    uint32_t clip_arrived[THC_MAX_WORKERS];    // ... and that wait for the norm (cleared by the last one that does)
+    uint32_t norm_counters[THC_MAX_WORKERS];   // norm of a list of tensors: CTAs that are done per worker (self-resetting)
 };
 
 // ------------------------------------------------------------------------ dependent launches

@@ -7,9 +7,12 @@
 // names its flat position, from which every address follows (the table of tensor addresses holds the address that
 // flat position 0 would have).
 //
-// Clipping needs the norm of everything before the first product.  One launch does both: sums of squares, a barrier
-// among the CTAs of a worker, products.  What a warp read last stays in shared memory (up to 8 KB a warp, 28 MB in all), the
-// rest is read again, backwards, because what was read last is still in L2.
+// Clipping needs the norm of everything before the first product.  Short lists take one launch, a cluster of CTAs per worker
+// that keeps what it reads in shared memory.  The others take two: sums of squares, whose last CTA forms norm and factor, then
+// products, eight pieces to a CTA and the last pieces first, which are still in L2.  (One launch for them too, with a barrier
+// of all CTAs in its middle, was not faster: a cooperative launch waits some 2 us longer for the one before it, and CTAs that stay
+// take their pieces further apart than the scheduler deals them out.  DRAM minds when reads and writes mix: 256 MiB fp32 to
+// another buffer 92 us with pieces in a fixed stride, 82 us with a CTA for each eight.)
 #include "thc_host.h"
 
 #include <algorithm>
@@ -25,8 +28,10 @@ namespace thc {
 constexpr uint32_t kPiece = 2048;              // elements of a piece: eight units of eight per lane
 constexpr uint32_t kUnit = 8;                  // consecutive elements of a lane: 16 bytes of a 16-bit type, 32 of fp32
 constexpr int kListThreads = 256, kListWarps = kListThreads / 32;
-constexpr uint32_t kNormCtasPerSm = 4, kClipCtasPerSm = 3;
-constexpr uint32_t kHeldBytes = 8192;          // per warp: a piece of fp32
+constexpr uint32_t kNormCtasPerSm = 4, kProductCtasPerSm = 3;
+constexpr int kClusterThreads = 512, kClusterWarps = kClusterThreads / 32;
+constexpr uint32_t kClusterCtas = 8;
+constexpr uint32_t kHeldBytes = 4096;          // per warp: half a piece of fp32, which is the most that a warp of the cluster takes at a time
 
 // {flat position (64 bits), tensor, length (16 bits) and type}
 struct Piece { uint64_t flat; uint32_t tensor, len_type; };
@@ -42,13 +47,16 @@ struct ListTable {
 // scale is 2^-126 and factor keeps all its bits: x scale is exact wherever c x is not itself a denormal.  Else scale is 1.
 struct Factor { float factor, scale; };
 __device__ __forceinline__ float times(const Factor &c, float x) { return c.factor * (x * c.scale); }
+__device__ __forceinline__ Factor factor_of(double norm, double max_norm)
+{
+    if (isinf(max_norm)) return Factor{1.0f, 1.0f};
+    const double c = max_norm / (norm + 1e-6);
+    if (c < 0x1p-126) return Factor{(float)(c * 0x1p126), 0x1p-126f};
+    return Factor{c > 1.0 ? 1.0f : (float)c, 1.0f};    // NaN stays
+}
 
-struct NormOut {
-    double *partial;             // [n][gridDim.x]
-    float *norms;                // or null
-    DeviceBlock *dev;
-    double max_norm;
-};
+// What the norm leaves for the products.
+struct alignas(16) NormResult { Factor c; float step_size, inv_sqrt_by2; uint32_t stop, pad_[3]; };
 
 __device__ __forceinline__ Piece load_piece(const Piece *p)
 {
@@ -67,15 +75,21 @@ __device__ __forceinline__ uint64_t load_base(const uint64_t *p)
 template <uint32_t T> struct Raw { uint32_t w[T == THC_F32 ? 8 : 4]; };
 template <uint32_t T> __host__ __device__ constexpr uint32_t size_of() { return T == THC_F32 ? 4u : 2u; }
 
-template <uint32_t T>
+// LAST: nothing reads it again, L2 may drop it first.
+template <uint32_t T, bool LAST = false>
 __device__ __forceinline__ Raw<T> load_unit8(uint64_t a)
 {
     Raw<T> r;
-    if constexpr (T == THC_F32)
-        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+    if constexpr (T == THC_F32 && LAST)
+        asm volatile("ld.global.L2::evict_first.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(a));
+    else if constexpr (T == THC_F32)
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(a));
+    else if constexpr (LAST)
+        asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(a));
     else
-        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(a));
+        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(a));
     return r;
 }
 
@@ -208,57 +222,16 @@ __device__ __forceinline__ double squares(const Piece &p, const uint64_t *base, 
 }
 
 // Sum over the CTA's threads, in thread 0.
-__device__ __forceinline__ double sum_of_cta(double s, double (&red)[kListWarps])
+template <int WARPS>
+__device__ __forceinline__ double sum_of_cta(double s, double (&red)[WARPS])
 {
     for (int off = 16; off > 0; off >>= 1) s += __shfl_down_sync(0xFFFFFFFFu, s, off);
     if ((threadIdx.x & 31u) == 0) red[threadIdx.x >> 5] = s;
     __syncthreads();
     double t = 0.0;
     if (threadIdx.x == 0)
-        for (int w = 0; w < kListWarps; ++w) t += red[w];
+        for (int w = 0; w < WARPS; ++w) t += red[w];
     return t;
-}
-
-__device__ __forceinline__ void report_norm(const NormOut &o, uint32_t worker, double norm)
-{
-    if (!isfinite(norm)) atomicOr(&o.dev->status, THC_STATUS_NONFINITE);
-    if (o.norms != nullptr) o.norms[worker] = (float)norm;
-}
-
-// Sums of squares of all pieces; a warp's pieces are fixed by the grid and the sums are added in a fixed order.
-__global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
-list_norm_kernel(const __grid_constant__ ListTable L, const __grid_constant__ NormOut o)
-{
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
-    const uint32_t stride = gridDim.x * kListWarps;
-    uint32_t c = blockIdx.x * kListWarps + warp;
-    Piece p{};
-    if (c < L.pieces_n) p = load_piece(L.pieces + c);   // written before any launch
-    depend_on_previous();
-    const uint64_t *base = L.base + (uint64_t)worker * L.count;
-    double s = 0.0;
-#pragma unroll 1
-    while (c < L.pieces_n) {
-        const Piece now = p;
-        c += stride;
-        if (c < L.pieces_n) p = load_piece(L.pieces + c);
-        s += squares<false>(now, base, 0, lane, kNotHeld);
-    }
-    __shared__ double red[kListWarps];
-    __shared__ uint32_t last;
-    double t = sum_of_cta(s, red);
-    if (threadIdx.x == 0) {
-        __stcg(o.partial + (uint64_t)worker * gridDim.x + blockIdx.x, t);
-        __threadfence();
-        last = atomicInc(o.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    t = 0.0;
-    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) t += __ldcg(o.partial + (uint64_t)worker * gridDim.x + i);
-    t = sum_of_cta(t, red);
-    if (threadIdx.x == 0) report_norm(o, worker, sqrt(t));
 }
 
 // ---------------------------------------------------------------------------------- products
@@ -409,18 +382,23 @@ __device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &
     }
 }
 
-// ---------------------------------------------------------------------------------- the calls that clip
+// ---------------------------------------------------------------------------------- the calls
 enum ClipKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter, kAdam, kAdamMaster };
+__host__ __device__ constexpr bool is_adam(ClipKind k) { return k == kAdam || k == kAdamMaster; }
 
-struct ClipParams {
+struct ListParams {
     ListTable L;                 // whose pieces are walked
-    const uint64_t *dst_base;    // kClip: addresses of the tensors that are written
-    NormOut o;
-    uint32_t with_norm;          // 0: no norm, factor 1
-    uint32_t split_log2;         // a warp takes a 2^-split_log2 of a piece at a time
+    uint32_t n;
+    uint32_t split_log2;         // a warp takes a 2^-split_log2 of a piece at a time: an item
     uint64_t src_flat;           // kScatter, kAdam*: what is read (else the tensors of L)
-    uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS];   // kGather*
+    const uint64_t *dst_base;    // kClip: addresses of the tensors that are written
+    double max_norm;
+    float *norms;                // or null: no norm, factor 1
+    double *partial;             // workspace: a sum per CTA
+    NormResult *result;          // workspace: one per worker
+    DeviceBlock *dev;
     AdamParams adam;
+    uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS];   // kGather*
 };
 
 // Part `item` of all parts of the pieces; length 0 where a piece is too short to have it.
@@ -433,13 +411,23 @@ __device__ __forceinline__ Piece load_item(const ListTable &L, uint32_t item, ui
     return p;
 }
 
+// The addresses that the products of an item need from the tables.
+struct ItemBase { uint64_t tensor, dst; };
+template <ClipKind K>
+__device__ __forceinline__ ItemBase load_item_base(const ListParams &P, const Piece &p, uint32_t worker)
+{
+    const uint64_t i = (uint64_t)worker * P.L.count + p.tensor;
+    return ItemBase{load_base(P.L.base + i), K == kClip ? load_base(P.dst_base + i) : 0};
+}
+
 template <ClipKind K, uint32_t T>
-__device__ __forceinline__ void move_typed(const ClipParams &P, const Piece &p, uint32_t worker, const Factor &c, uint32_t lane, uint32_t held)
+__device__ __forceinline__ void move_typed(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t worker, const Factor &c, uint32_t lane,
+                                           uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu;
-    const uint64_t i = (uint64_t)worker * P.L.count + p.tensor, at = p.flat * size_of<T>(), tensor = load_base(P.L.base + i) + at;
+    const uint64_t at = p.flat * size_of<T>(), tensor = base.tensor + at;
     if (K == kClip) {
-        move_piece<T, T, false>(tensor, load_base(P.dst_base + i) + at, 0, len, len, c, lane, held);
+        move_piece<T, T, false>(tensor, base.dst + at, 0, len, len, c, lane, held);
     } else if (K == kScatter) {
         move_piece<THC_F32, T, false>(P.src_flat + p.flat * 4u, tensor, 0, len, len, c, lane, held);
     } else {
@@ -450,135 +438,201 @@ __device__ __forceinline__ void move_typed(const ClipParams &P, const Piece &p, 
     }
 }
 
-// Waits until all CTAs of the worker have added themselves to `arrived`; false if that takes some seconds (it cannot: the
-// launch is cooperative, so all of them run).
-__device__ __forceinline__ bool wait_for(const uint32_t *arrived, uint32_t ctas)
+template <ClipKind K>
+__device__ __forceinline__ void products(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t worker, AdamStep &k, float lr,
+                                         uint32_t lane, uint32_t held)
 {
-    for (uint32_t i = 0; i < (1u << 23); ++i) {
-        uint32_t v;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
-        if (v >= ctas) return true;
+    const uint32_t type = p.len_type >> 16;
+    if constexpr (K == kAdam || K == kAdamMaster) {
+        const double wd = P.adam.decay != nullptr ? (double)ld_global(P.adam.decay + p.tensor) : P.adam.weight_decay;
+        k.keep = (float)(1.0 - (double)lr * wd);
+        if (K == kAdam || type == THC_F32) adam_piece<THC_F32, K == kAdamMaster>(P.adam, k, p, base.tensor, lane, held);
+        else if (type == THC_BF16) adam_piece<THC_BF16, K == kAdamMaster>(P.adam, k, p, base.tensor, lane, held);
+        else adam_piece<THC_F16, K == kAdamMaster>(P.adam, k, p, base.tensor, lane, held);
+    } else {
+        if (type == THC_F32) move_typed<K, THC_F32>(P, p, base, worker, k.c, lane, held);
+        else if (type == THC_BF16) move_typed<K, THC_BF16>(P, p, base, worker, k.c, lane, held);
+        else move_typed<K, THC_F16>(P, p, base, worker, k.c, lane, held);
     }
-    return false;
 }
 
-// grid (CTAs of a worker, workers).  Phase 1: squares of the worker's pieces; the sums meet in the workspace, every CTA adds
-// all of them in the same order and forms norm and factor itself (one that did it for all would cost the others two
-// more trips to L2).  Phase 2: the products, the held pieces first.
-template <ClipKind K>
-__global__ void __launch_bounds__(kListThreads, kClipCtasPerSm)
-list_clip_kernel(const __grid_constant__ ClipParams P)
+// The constants of the Adam step that do not depend on the norm.
+__device__ __forceinline__ void adam_constants(const AdamParams &a, AdamStep &k)
 {
-    constexpr bool kIsAdam = K == kAdam || K == kAdamMaster;
-    extern __shared__ __align__(16) unsigned char held_bytes[];
-    __shared__ double red[kListWarps];
-    __shared__ AdamStep s_step;
-    __shared__ uint32_t s_go;
+    k.b1 = (float)a.beta1;
+    k.b2 = (float)a.beta2;
+    k.a1 = (float)(1.0 - a.beta1);
+    k.a2 = (float)(1.0 - a.beta2);
+    k.eps = (float)a.eps;
+}
+// Those that depend on the step count t (in the norm's result: step_size, inv_sqrt_by2).
+__device__ __forceinline__ void adam_sizes(const AdamParams &a, float lr, int64_t t, float *step_size, float *inv_sqrt_by2)
+{
+    *step_size = (float)((double)lr / (1.0 - pow(a.beta1, (double)t)));
+    *inv_sqrt_by2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
+}
+
+// Norm to the caller, factor to the products.  ADAM: also the step count, unless the norm is not finite.
+template <bool ADAM>
+__device__ __forceinline__ NormResult finish_norm(const ListParams &P, uint32_t worker, double sum)
+{
+    const double norm = sqrt(sum);
+    NormResult r{};
+    r.c = factor_of(norm, P.max_norm);
+    P.norms[worker] = (float)norm;
+    if (!isfinite(norm)) {
+        atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
+        r.stop = 1u;
+    } else if (ADAM) {
+        const int64_t t = *P.adam.step + 1;
+        *P.adam.step = t;
+        adam_sizes(P.adam, *P.adam.lr, t, &r.step_size, &r.inv_sqrt_by2);
+    }
+    return r;
+}
+
+// Sums of squares, grid (CTAs of a worker, workers).  A warp's pieces are fixed by the grid and the sums are added in a fixed
+// order; a worker's last CTA does that.
+template <bool ADAM>
+__global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
+list_norm_kernel(const __grid_constant__ ListParams P)
+{
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
-    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(held_bytes) + warp * kHeldBytes;
     const uint32_t stride = gridDim.x * kListWarps, items = P.L.pieces_n << P.split_log2;
-    const uint32_t first = blockIdx.x * kListWarps + warp;
-    const uint32_t mine = first < items ? (items - first + stride - 1u) / stride : 0u;
-    uint32_t in_slot = 0;                              // items of the warp that are held: its last one, or two of 16 bits
+    uint32_t c = blockIdx.x * kListWarps + warp;
+    Piece p{};
+    if (c < items) p = load_item(P.L, c, P.split_log2);     // written before any launch
     depend_on_previous();
+    const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
+    double s = 0.0;
+#pragma unroll 1
+    while (c < items) {
+        const Piece now = p;
+        c += stride;
+        if (c < items) p = load_item(P.L, c, P.split_log2);
+        s += squares<false>(now, base, P.src_flat, lane, kNotHeld);
+    }
+    __shared__ double red[kListWarps];
+    __shared__ uint32_t last;
+    double t = sum_of_cta(s, red);
+    if (threadIdx.x == 0) {
+        __stcg(P.partial + (uint64_t)worker * gridDim.x + blockIdx.x, t);
+        __threadfence();
+        last = atomicInc(P.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    t = 0.0;
+    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) t += __ldcg(P.partial + (uint64_t)worker * gridDim.x + i);
+    t = sum_of_cta(t, red);
+    if (threadIdx.x == 0) {
+        const NormResult r = finish_norm<ADAM>(P, worker, t);
+        if (P.result != nullptr) P.result[worker] = r;
+    }
+}
+
+// Products of eight items to a CTA, over all workers; the last ones first.
+template <ClipKind K>
+__global__ void __launch_bounds__(kListThreads, kProductCtasPerSm)
+list_product_kernel(const __grid_constant__ ListParams P)
+{
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t items = P.L.pieces_n << P.split_log2, all = items * P.n, j = blockIdx.x * kListWarps + warp;
+    if (j >= all) return;
+    const uint32_t at = all - 1u - j, worker = at / items;
+    const Piece p = load_item(P.L, at % items, P.split_log2);
+    depend_on_previous();
+    const ItemBase base = load_item_base<K>(P, p, worker);
     AdamStep k{};
     k.c = Factor{1.0f, 1.0f};
     float lr = 0.0f;
-    if (kIsAdam) lr = ld_global(P.adam.lr);
-    if (P.with_norm != 0u) {
-        const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
-        constexpr bool kFlat = kIsAdam || K == kScatter;
-        double s = 0.0;
-        Piece p{};
-        if (mine != 0u) p = load_item(P.L, first, P.split_log2);
-#pragma unroll 1
-        for (uint32_t i = 0; i < mine; ++i) {
-            const Piece now = p;
-            if (i + 1u < mine) p = load_item(P.L, first + (i + 1u) * stride, P.split_log2);
-            uint32_t held = kNotHeld;
-            if (i + 1u == mine) {
-                held = slot;                           // over the one before it unless both are of 16 bits
-                in_slot = in_slot != 0u && (now.len_type >> 16) != THC_F32 ? 2u : 1u;
-            } else if (!kFlat && i + 2u == mine && (now.len_type >> 16) != THC_F32) {
-                held = slot + kHeldBytes / 2;
-                in_slot = 1u;
-            }
-            s += squares<true>(now, base, kFlat ? P.src_flat : 0, lane, held);
+    if (P.norms != nullptr) {
+        const uint4 q = ld_global(reinterpret_cast<const uint4 *>(P.result + worker));
+        k.c = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
+        if (is_adam(K)) {
+            if (ld_global(&P.result->stop) != 0u) return;   // the norm is not finite
+            k.step_size = __uint_as_float(q.z);
+            k.inv_sqrt_by2 = __uint_as_float(q.w);
+            lr = ld_global(P.adam.lr);
+            adam_constants(P.adam, k);
         }
-        // what the Adam step needs of its count, before the wait
-        double step_size = 0.0, by2 = 0.0;
-        int64_t t = 0;
-        if (kIsAdam && threadIdx.x == 0) {
-            t = (int64_t)load_base(reinterpret_cast<const uint64_t *>(P.adam.step)) + 1;
-            step_size = (double)lr / (1.0 - pow(P.adam.beta1, (double)t));
-            by2 = 1.0 / sqrt(1.0 - pow(P.adam.beta2, (double)t));
-        }
-        double sum = sum_of_cta(s, red);
-        uint32_t *arrived = P.o.dev->clip_arrived + worker, *left = P.o.dev->norm_counters + worker;
-        const double *partial = P.o.partial + (uint64_t)worker * gridDim.x;
-        if (threadIdx.x == 0) {
-            __stcg(P.o.partial + (uint64_t)worker * gridDim.x + blockIdx.x, sum);
-            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" :: "l"(arrived) : "memory");
-            s_go = wait_for(arrived, gridDim.x) ? 1u : 0u;
-            // the last one to leave clears the counter for the next launch
-            if (atomicInc(left, gridDim.x - 1u) == gridDim.x - 1u) atomicExch(arrived, 0u);
-        }
-        __syncthreads();
-        if (s_go == 0u) {
-            if (threadIdx.x == 0) atomicOr(&P.o.dev->status, THC_STATUS_WAIT_TIMEOUT);
-            return;
-        }
-        sum = 0.0;
-        for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(partial + i);
-        sum = sum_of_cta(sum, red);
-        if (threadIdx.x == 0) {
-            const double norm = sqrt(sum);
-            if (blockIdx.x == 0) report_norm(P.o, worker, norm);
-            Factor c{1.0f, 1.0f};
-            if (!isinf(P.o.max_norm)) {
-                const double f = P.o.max_norm / (norm + 1e-6);
-                if (f < 0x1p-126) c = Factor{(float)(f * 0x1p126), 0x1p-126f};
-                else c.factor = f > 1.0 ? 1.0f : (float)f;   // NaN stays
-            }
-            s_step.c = c;
-            if (kIsAdam) {
-                if (!isfinite(norm)) s_go = 0u;        // no step
-                else if (blockIdx.x == 0) *P.adam.step = t;
-                s_step.step_size = (float)step_size;
-                s_step.inv_sqrt_by2 = (float)by2;
-            }
-        }
-        __syncthreads();
-        if (s_go == 0u) return;
-        k = s_step;
     }
-    if (kIsAdam) {
-        k.b1 = (float)P.adam.beta1;
-        k.b2 = (float)P.adam.beta2;
-        k.a1 = (float)(1.0 - P.adam.beta1);
-        k.a2 = (float)(1.0 - P.adam.beta2);
-        k.eps = (float)P.adam.eps;
+    products<K>(P, p, base, worker, k, lr, lane, kNotHeld);
+}
+
+// Both in one launch, grid (8 CTAs, workers), a cluster per worker.  The CTAs' sums are written to all CTAs' shared memory;
+// each adds them in the same order and forms norm and factor itself.  A warp's last item is still in its shared memory.
+template <ClipKind K>
+__global__ void __launch_bounds__(kClusterThreads, 1)
+list_cluster_kernel(const __grid_constant__ ListParams P)
+{
+    extern __shared__ __align__(16) unsigned char held_bytes[];
+    __shared__ double red[kClusterWarps], sums[kClusterCtas];
+    __shared__ NormResult s_result;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
+    const uint32_t held = (uint32_t)__cvta_generic_to_shared(held_bytes) + warp * kHeldBytes;
+    const uint32_t stride = kClusterCtas * kClusterWarps, items = P.L.pieces_n << P.split_log2, first = blockIdx.x * kClusterWarps + warp;
+    uint32_t c = first;
+    Piece last{}, p{};
+    ItemBase last_base{};
+    if (c < items) p = load_item(P.L, c, P.split_log2);     // written before any launch
+    depend_on_previous();
+    const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
+    AdamStep k{};
+    int64_t t = 0;
+    float lr = 0.0f;
+    if (is_adam(K)) {
+        adam_constants(P.adam, k);
+        lr = ld_global(P.adam.lr);
+        t = (int64_t)load_base(reinterpret_cast<const uint64_t *>(P.adam.step)) + 1;
     }
-    Piece p{};
-    if (mine != 0u) p = load_item(P.L, first + (mine - 1u) * stride, P.split_log2);
+    double s = 0.0;
 #pragma unroll 1
-    for (uint32_t i = mine; i-- > 0u;) {
-        const Piece now = p;
-        if (i > 0u) p = load_item(P.L, first + (i - 1u) * stride, P.split_log2);
-        const uint32_t back = mine - 1u - i, held = back < in_slot ? slot + back * (kHeldBytes / 2) : kNotHeld;
-        const uint32_t type = now.len_type >> 16;
-        if constexpr (kIsAdam) {
-            const double wd = P.adam.decay != nullptr ? (double)ld_global(P.adam.decay + now.tensor) : P.adam.weight_decay;
-            k.keep = (float)(1.0 - (double)lr * wd);
-            const uint64_t tensor = load_base(P.L.base + now.tensor);
-            if (K == kAdam || type == THC_F32) adam_piece<THC_F32, K == kAdamMaster>(P.adam, k, now, tensor, lane, held);
-            else if (type == THC_BF16) adam_piece<THC_BF16, K == kAdamMaster>(P.adam, k, now, tensor, lane, held);
-            else adam_piece<THC_F16, K == kAdamMaster>(P.adam, k, now, tensor, lane, held);
-        } else {
-            if (type == THC_F32) move_typed<K, THC_F32>(P, now, worker, k.c, lane, held);
-            else if (type == THC_BF16) move_typed<K, THC_BF16>(P, now, worker, k.c, lane, held);
-            else move_typed<K, THC_F16>(P, now, worker, k.c, lane, held);
+    for (; c < items; c += stride) {
+        last = p;
+        if (c + stride < items) p = load_item(P.L, c + stride, P.split_log2);
+        else last_base = load_item_base<K>(P, last, worker);
+        s += squares<true>(last, base, P.src_flat, lane, c + stride < items ? kNotHeld : held);
+    }
+    const double sum = sum_of_cta(s, red);
+    if (threadIdx.x == 0) {
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x]);
+#pragma unroll
+        for (uint32_t r = 0; r < kClusterCtas; ++r)
+            asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f64 [a], %2;\n\t}" :: "r"(to), "r"(r), "d"(sum) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (is_adam(K) && threadIdx.x == 0) adam_sizes(P.adam, lr, t, &s_result.step_size, &s_result.inv_sqrt_by2);
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x == 0) {
+        double total = 0.0;
+#pragma unroll
+        for (uint32_t r = 0; r < kClusterCtas; ++r) total += sums[r];
+        const double norm = sqrt(total);
+        s_result.c = factor_of(norm, P.max_norm);
+        s_result.stop = isfinite(norm) ? 0u : 1u;
+        if (blockIdx.x == 0) {
+            P.norms[worker] = (float)norm;
+            if (!isfinite(norm)) atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
+            else if (is_adam(K)) *P.adam.step = t;     // every CTA has read it before the barrier
         }
+    }
+    __syncthreads();
+    if (is_adam(K)) {
+        if (s_result.stop != 0u) return;
+        k.step_size = s_result.step_size;
+        k.inv_sqrt_by2 = s_result.inv_sqrt_by2;
+    }
+    k.c = s_result.c;
+    if (first >= items) return;
+    const uint32_t final = first + (items - 1u - first) / stride * stride;
+    products<K>(P, last, last_base, worker, k, lr, lane, held);
+#pragma unroll 1
+    for (c = final; c >= stride; ) {
+        c -= stride;
+        p = load_item(P.L, c, P.split_log2);
+        products<K>(P, p, load_item_base<K>(P, p, worker), worker, k, lr, lane, kNotHeld);
     }
 }
 
@@ -600,7 +654,7 @@ struct thc_tensors {
     int device;                                // -1: host only
     uint32_t n, count, pieces_n, sm_count;
     uint64_t d, elements;
-    bool all_f32;
+    bool all_f32;                              // the tensors that are not empty
     std::vector<uint64_t> numel, offset;
     std::vector<uint32_t> dtype;
     std::vector<uint64_t> address;             // [n][count]
@@ -670,7 +724,7 @@ int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uin
         if (d > (1ull << 40)) return THC_EINVAL;
     }
     if (elements == 0) return THC_EINVAL;
-    if (pieces_n > 0x7FFFFFFFull) return THC_EUNSUPPORTED;
+    if (pieces_n * n > 0x7FFFFFFFull) return THC_EUNSUPPORTED;
     thc_tensors *h = nullptr;
     try {
         h = new thc_tensors;
@@ -692,7 +746,7 @@ int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uin
         for (uint32_t t = 0; t < count; ++t) {
             h->offset[t] = at;
             at += (numel[t] + THC_TENSOR_ALIGN - 1) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
-            if (dtype[t] != THC_F32 && numel[t] != 0) h->all_f32 = false;
+            if (numel[t] != 0 && dtype[t] != THC_F32) h->all_f32 = false;
         }
         const int rc = take_addresses(h, tensors);
         if (rc != THC_OK) { delete h; return rc; }
@@ -731,19 +785,19 @@ int thc_tensors_destroy(thc_tensors *h)
     return THC_OK;
 }
 
-// CTAs per worker of a launch over all pieces, each cut into 2^split_log2 parts.
-static uint32_t ctas_of(const thc_tensors *h, uint32_t per_sm, uint32_t split_log2 = 0)
+// CTAs per worker of the sums.
+static uint32_t norm_ctas(const thc_tensors *h, uint32_t split_log2)
 {
-    const uint32_t most = std::max(1u, h->sm_count * per_sm / h->n);
+    const uint32_t most = std::max(1u, h->sm_count * kNormCtasPerSm / h->n);
     return (uint32_t)std::min<uint64_t>(most, (((uint64_t)h->pieces_n << split_log2) + kListWarps - 1) / kListWarps);
 }
 
 static uint64_t round_up256(uint64_t v) { return (v + 255) / 256 * 256; }
 
-// Workspace: the partial sums.
+// Workspace: results of the workers, then the sums' partial results.
 static uint64_t workspace_need(const thc_tensors *h)
 {
-    return round_up256((uint64_t)h->n * std::max(1u, h->sm_count * std::max(kNormCtasPerSm, kClipCtasPerSm) / h->n) * sizeof(double));
+    return round_up256(h->n * sizeof(NormResult)) + round_up256((uint64_t)h->n * norm_ctas(h, 3) * sizeof(double));
 }
 
 int thc_tensors_sizes(const thc_tensors *h, thc_tensors_sizes_t *s)
@@ -826,15 +880,30 @@ static bool overlaps(const thc_tensors *h, uint64_t lo, uint64_t hi)
     return it != h->ranges.end() && it->lo < hi;
 }
 
-static NormOut norm_out(const CtxView &v, double max_norm, float *norms, void *workspace)
+// A piece is eight units of a lane, one after the other or four at a time: few pieces are cut so that more warps share them.
+static uint32_t split_of(const thc_tensors *h, uint64_t warps)
 {
-    NormOut o;
-    memset(&o, 0, sizeof o);
-    o.partial = static_cast<double *>(workspace);
-    o.norms = norms;
-    o.dev = v.dev;
-    o.max_norm = max_norm;
-    return o;
+    uint32_t split = 0;
+    while (split < 3 && ((uint64_t)h->pieces_n << (split + 1)) <= warps) ++split;
+    return split;
+}
+
+static void fill_params(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace)
+{
+    P.L = table_of(h);
+    P.n = h->n;
+    P.max_norm = max_norm;
+    P.norms = norms;
+    P.result = static_cast<NormResult *>(workspace);
+    P.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + round_up256(h->n * sizeof(NormResult)));
+    P.dev = view_of(ctx).dev;
+}
+
+static int launch_norm(ListParams &P, const thc_tensors *h, void (*kern)(ListParams), cudaStream_t st)
+{
+    P.split_log2 = split_of(h, (uint64_t)h->sm_count * kListWarps / h->n);
+    THC_CUDA(launch_after(kern, dim3(norm_ctas(h, P.split_log2), h->n), kListThreads, 0, st, P));
+    return THC_OK;
 }
 
 int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes, void *stream)
@@ -843,41 +912,50 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
     if (rc != THC_OK) return rc;
     if (norms == nullptr || !aligned4(norms)) return THC_EINVAL;
     if ((rc = check_workspace(list, workspace, workspace_bytes)) != THC_OK) return rc;
-    THC_CUDA(launch_after(list_norm_kernel, dim3(ctas_of(list, kNormCtasPerSm), list->n), kListThreads, 0, static_cast<cudaStream_t>(stream),
-                          table_of(list), norm_out(view_of(ctx), INFINITY, norms, workspace)));
-    return THC_OK;
+    ListParams P;
+    memset(&P, 0, sizeof P);
+    fill_params(P, ctx, list, INFINITY, norms, workspace);
+    P.result = nullptr;
+    return launch_norm(P, list, list_norm_kernel<false>, static_cast<cudaStream_t>(stream));
 }
 
-// One launch of list_clip_kernel; cooperative where its CTAs wait for one another.
-static int launch_clip(thc_ctx *ctx, void (*kern)(ClipParams), ClipParams &P, const thc_tensors *h, double max_norm, float *norms,
-                       void *workspace, cudaStream_t st)
+// Lists of at most this many pieces a worker take the cluster.
+constexpr uint32_t kClusterMostPieces = 256;
+
+template <ClipKind K>
+static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace, void *stream)
 {
-    P.L = table_of(h);
-    P.with_norm = norms != nullptr ? 1u : 0u;
-    P.o = norm_out(view_of(ctx), max_norm, norms, workspace);
-    // A piece is eight units a lane, one after the other or four at a time: few pieces are cut so that more warps share them.
-    P.split_log2 = 0;
-    while (P.split_log2 < 3 && ((uint64_t)h->pieces_n * h->n << (P.split_log2 + 1)) <= (uint64_t)h->sm_count * kClipCtasPerSm * kListWarps) ++P.split_log2;
-    const uint32_t smem = kHeldBytes * kListWarps;
-    const int rc = ensure_dynamic_smem(reinterpret_cast<const void *>(kern));
-    if (rc != THC_OK) return rc;
-    cudaLaunchAttribute attr;
-    if (P.with_norm) {
-        attr.id = cudaLaunchAttributeCooperative;
-        attr.val.cooperative = 1;
-    } else {
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    fill_params(P, ctx, h, max_norm, norms, workspace);
+    if (norms != nullptr && h->pieces_n <= kClusterMostPieces) {
+        P.split_log2 = std::max(1u, split_of(h, kClusterCtas * kClusterWarps));   // (1: see kHeldBytes)
+        const void *kern = reinterpret_cast<const void *>(list_cluster_kernel<K>);
+        const int rc = ensure_dynamic_smem(kern);
+        if (rc != THC_OK) return rc;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = kClusterCtas;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof cfg);
+        cfg.gridDim = dim3(kClusterCtas, h->n);
+        cfg.blockDim = dim3(kClusterThreads);
+        cfg.dynamicSmemBytes = kHeldBytes * kClusterWarps;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        THC_CUDA(cudaLaunchKernelEx(&cfg, list_cluster_kernel<K>, P));
+        return THC_OK;
     }
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3(ctas_of(h, kClipCtasPerSm, P.split_log2), h->n);
-    cfg.blockDim = dim3(kListThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    THC_CUDA(cudaLaunchKernelEx(&cfg, kern, P));
+    if (norms != nullptr) {
+        const int rc = launch_norm(P, h, list_norm_kernel<is_adam(K)>, st);
+        if (rc != THC_OK) return rc;
+    }
+    P.split_log2 = split_of(h, (uint64_t)h->sm_count * kProductCtasPerSm * kListWarps / h->n);
+    const uint64_t items = ((uint64_t)h->pieces_n << P.split_log2) * h->n;
+    THC_CUDA(launch_after(list_product_kernel<K>, dim3((unsigned)((items + kListWarps - 1) / kListWarps)), kListThreads, 0, st, P));
     return THC_OK;
 }
 
@@ -907,10 +985,10 @@ int thc_clip_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const
             if (overlaps(out, r.lo, r.hi)) return THC_EINVAL;
         }
     }
-    ClipParams P;
+    ListParams P;
     memset(&P, 0, sizeof P);
     P.dst_base = out->base;
-    return launch_clip(ctx, list_clip_kernel<kClip>, P, list, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+    return launch_call<kClip>(P, ctx, list, max_norm, norms, workspace, stream);
 }
 
 int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *const *ef_or_null, void *const *flats,
@@ -923,7 +1001,7 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
     if (bf16 && ef_or_null != nullptr) return THC_EUNSUPPORTED;
     if (flats == nullptr) return THC_EINVAL;
     const uint64_t bytes = list->d * (bf16 ? 2u : 4u);
-    ClipParams P;
+    ListParams P;
     memset(&P, 0, sizeof P);
     for (uint32_t i = 0; i < list->n; ++i) {
         if (flats[i] == nullptr || !aligned16(flats[i])) return THC_EINVAL;
@@ -941,8 +1019,9 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
             if (ef_or_null != nullptr && !(j == i && P.ef[j] == P.dst_flat[i]) && !apart(P.dst_flat[i], P.ef[j])) return THC_EINVAL;
         }
     }
-    return launch_clip(ctx, ef_or_null != nullptr ? list_clip_kernel<kGatherResidual> : bf16 ? list_clip_kernel<kGatherBf16> : list_clip_kernel<kGatherF32>,
-                       P, list, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+    if (ef_or_null != nullptr) return launch_call<kGatherResidual>(P, ctx, list, max_norm, norms, workspace, stream);
+    if (bf16) return launch_call<kGatherBf16>(P, ctx, list, max_norm, norms, workspace, stream);
+    return launch_call<kGatherF32>(P, ctx, list, max_norm, norms, workspace, stream);
 }
 
 int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const thc_tensors *list, float *norms, void *workspace,
@@ -955,10 +1034,10 @@ int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const th
     const uint64_t lo = reinterpret_cast<uint64_t>(flat), hi = lo + list->d * 4u;
     for (const auto &r : list->ranges)
         if (r.lo < hi && lo < r.hi && !(list->dtype[r.index] == THC_F32 && r.lo == lo + list->offset[r.index] * 4u)) return THC_EINVAL;
-    ClipParams P;
+    ListParams P;
     memset(&P, 0, sizeof P);
     P.src_flat = lo;
-    return launch_clip(ctx, list_clip_kernel<kScatter>, P, list, max_norm, norms, workspace, static_cast<cudaStream_t>(stream));
+    return launch_call<kScatter>(P, ctx, list, max_norm, norms, workspace, stream);
 }
 
 int thc_adamw(thc_ctx *ctx, const thc_adamw_config *cfg, const float *grad, const thc_tensors *list, const float *lr, int64_t *step,
@@ -985,10 +1064,10 @@ int thc_adamw(thc_ctx *ctx, const thc_adamw_config *cfg, const float *grad, cons
             if (a < b + bytes && b < a + bytes) return THC_EINVAL;
         }
     }
-    ClipParams P;
+    ListParams P;
     memset(&P, 0, sizeof P);
     P.src_flat = reinterpret_cast<uint64_t>(grad);
     P.adam = AdamParams{grad, master_or_null, m, v, lr, decay_or_null, step, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay};
-    return launch_clip(ctx, master_or_null != nullptr ? list_clip_kernel<kAdamMaster> : list_clip_kernel<kAdam>, P, list, cfg->max_norm, norms,
-                       workspace, static_cast<cudaStream_t>(stream));
+    if (master_or_null != nullptr) return launch_call<kAdamMaster>(P, ctx, list, cfg->max_norm, norms, workspace, stream);
+    return launch_call<kAdam>(P, ctx, list, cfg->max_norm, norms, workspace, stream);
 }
