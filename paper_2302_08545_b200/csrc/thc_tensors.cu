@@ -28,7 +28,7 @@ namespace thc {
 constexpr uint32_t kPiece = 2048;              // elements of a piece: eight units of eight per lane
 constexpr uint32_t kUnit = 8;                  // consecutive elements of a lane: 16 bytes of a 16-bit type, 32 of fp32
 constexpr int kListThreads = 256, kListWarps = kListThreads / 32;
-constexpr uint32_t kNormCtasPerSm = 4, kProductCtasPerSm = 3;
+constexpr uint32_t kNormCtasPerSm = 4;
 constexpr int kClusterThreads = 512, kClusterWarps = kClusterThreads / 32;
 constexpr uint32_t kClusterCtas = 8;
 constexpr uint32_t kHeldBytes = 4096;          // per warp: half a piece of fp32, which is the most that a warp of the cluster takes at a time
@@ -331,60 +331,83 @@ __device__ __forceinline__ float adam(const AdamStep &k, float g, float &m, floa
     return fmaf(-k.step_size, move, w * k.keep);
 }
 
-template <uint32_t T, bool MASTER>
-__device__ __forceinline__ void adam_piece(const AdamParams &P, const AdamStep &k, const Piece &p, uint64_t tensor, uint32_t lane, uint32_t held)
+// Where an item's operands are.  The tensor itself is read and written in units if it is aligned for them, else by element.
+struct AdamPlace { uint64_t g, m, v, w, out; uint32_t len, units; bool w_units; };
+template <bool MASTER>
+__device__ __forceinline__ AdamPlace adam_place(const AdamParams &P, const Piece &p, uint64_t tensor)
 {
-    const uint32_t len = p.len_type & 0xFFFFu;
     const uint64_t at = p.flat * 4u;
-    const uint64_t g = reinterpret_cast<uint64_t>(P.grad) + at, m = reinterpret_cast<uint64_t>(P.m) + at,
-                   v = reinterpret_cast<uint64_t>(P.v) + at, out = tensor + p.flat * size_of<T>();
-    const uint64_t w = MASTER ? reinterpret_cast<uint64_t>(P.master) + at : out;
-    uint32_t done = 0;
-    if (((g | m | v) & 31u) == 0 && (!MASTER || (w & 31u) == 0)) {
-        const bool whole = head_of<T>(out) == 0u;      // the tensor too takes units, else elements
-        const uint32_t units = len / kUnit;
-        done = units * kUnit;
-        uint32_t row = 0;
+    AdamPlace a;
+    a.g = reinterpret_cast<uint64_t>(P.grad) + at;
+    a.m = reinterpret_cast<uint64_t>(P.m) + at;
+    a.v = reinterpret_cast<uint64_t>(P.v) + at;
+    a.out = tensor + p.flat * ((p.len_type >> 16) == THC_F32 ? 4u : 2u);
+    a.w = MASTER ? reinterpret_cast<uint64_t>(P.master) + at : a.out;
+    a.len = p.len_type & 0xFFFFu;
+    a.w_units = (a.w & 31u) == 0;
+    a.units = ((a.g | a.m | a.v) & 31u) == 0 && (!MASTER || a.w_units) ? a.len / kUnit : 0u;
+    return a;
+}
+
+struct AdamUnit { Raw<THC_F32> g, m, v, w; };
+template <bool MASTER>
+__device__ __forceinline__ AdamUnit adam_load(const AdamPlace &a, uint32_t u, uint32_t held, uint32_t lane)
+{
+    const uint64_t o = (uint64_t)u * (kUnit * 4u);
+    AdamUnit r;
+    r.m = load_unit8<THC_F32>(a.m + o);
+    r.v = load_unit8<THC_F32>(a.v + o);
+    if (MASTER || a.w_units) r.w = load_unit8<THC_F32>(a.w + o);
+    else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.w.w[e] = ld_global(reinterpret_cast<const uint32_t *>(a.w + o + 4u * e));
+    r.g = held != kNotHeld ? held_unit<THC_F32>(held, u / 32u, lane) : load_unit8<THC_F32>(a.g + o);
+    return r;
+}
+
+// The step of an item; `cur` is the lane's first unit, if it has one.
+template <uint32_t T, bool MASTER>
+__device__ __forceinline__ void adam_item(const AdamPlace &a, const AdamStep &k, AdamUnit cur, uint32_t lane, uint32_t held)
+{
+    const bool whole = head_of<T>(a.out) == 0u;
 #pragma unroll 1
-        for (uint32_t u = lane; u < units; u += 32u, ++row) {
-            const uint64_t o = (uint64_t)u * (kUnit * 4u), to = out + (uint64_t)u * (kUnit * size_of<T>());
-            const Raw<THC_F32> rm = load_unit8<THC_F32>(m + o), rv = load_unit8<THC_F32>(v + o);
-            Raw<THC_F32> rw;
-            if (MASTER || whole) rw = load_unit8<THC_F32>(w + o);
-            else
+    for (uint32_t u = lane; u < a.units; u += 32u) {
+        const uint64_t o = (uint64_t)u * (kUnit * 4u), to = a.out + (uint64_t)u * (kUnit * size_of<T>());
+        AdamUnit next{};
+        if (u + 32u < a.units) next = adam_load<MASTER>(a, u + 32u, held, lane);
+        float ym[8], yv[8], yw[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) rw.w[e] = ld_global(reinterpret_cast<const uint32_t *>(w + o + 4u * e));
-            const Raw<THC_F32> rg = held != kNotHeld ? held_unit<THC_F32>(held, row, lane) : load_unit8<THC_F32>(g + o);
-            float ym[8], yv[8], yw[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ym[e] = value<THC_F32>(rm, e);
-                yv[e] = value<THC_F32>(rv, e);
-                yw[e] = adam(k, value<THC_F32>(rg, e), ym[e], yv[e], value<THC_F32>(rw, e));
-            }
-            store_unit8<THC_F32>(m + o, ym);
-            store_unit8<THC_F32>(v + o, yv);
-            if (MASTER) store_unit8<THC_F32>(w + o, yw);
-            if (whole) store_unit8<T>(to, yw);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) store_one<T>(to + size_of<T>() * e, yw[e]);
+        for (int e = 0; e < 8; ++e) {
+            ym[e] = value<THC_F32>(cur.m, e);
+            yv[e] = value<THC_F32>(cur.v, e);
+            yw[e] = adam(k, value<THC_F32>(cur.g, e), ym[e], yv[e], value<THC_F32>(cur.w, e));
         }
+        store_unit8<THC_F32>(a.m + o, ym);
+        store_unit8<THC_F32>(a.v + o, yv);
+        if (MASTER) store_unit8<THC_F32>(a.w + o, yw);
+        if (whole) store_unit8<T>(to, yw);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) store_one<T>(to + size_of<T>() * e, yw[e]);
+        cur = next;
     }
-    for (uint32_t j = done + lane; j < len; j += 32u) {
+    for (uint32_t j = a.units * kUnit + lane; j < a.len; j += 32u) {
         const uint64_t o = (uint64_t)j * 4u;
-        float ym = load_one<THC_F32>(m + o), yv = load_one<THC_F32>(v + o);
-        const float yw = adam(k, load_one<THC_F32>(g + o), ym, yv, load_one<THC_F32>(w + o));
-        store_one<THC_F32>(m + o, ym);
-        store_one<THC_F32>(v + o, yv);
-        if (MASTER) store_one<THC_F32>(w + o, yw);
-        store_one<T>(out + (uint64_t)j * size_of<T>(), yw);
+        float ym = load_one<THC_F32>(a.m + o), yv = load_one<THC_F32>(a.v + o);
+        const float yw = adam(k, load_one<THC_F32>(a.g + o), ym, yv, load_one<THC_F32>(a.w + o));
+        store_one<THC_F32>(a.m + o, ym);
+        store_one<THC_F32>(a.v + o, yv);
+        if (MASTER) store_one<THC_F32>(a.w + o, yw);
+        store_one<T>(a.out + (uint64_t)j * size_of<T>(), yw);
     }
 }
 
 // ---------------------------------------------------------------------------------- the calls
 enum ClipKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter, kAdam, kAdamMaster };
 __host__ __device__ constexpr bool is_adam(ClipKind k) { return k == kAdam || k == kAdamMaster; }
+// CTAs of list_product_kernel on an SM, by registers.  us with 2, 3, 4: 8 x 25.6M fp32 gathered 243, 242, 249; 355M scattered to
+// bf16 306, 305, 312; 138M bf16 clipped -, 141, 135; Adam step of 138M (two units at a time only with 2) 735, 806, -.
+__host__ __device__ constexpr int product_ctas_per_sm(ClipKind k) { return is_adam(k) ? 2 : k == kClip ? 4 : 3; }
 
 struct ListParams {
     ListTable L;                 // whose pieces are walked
@@ -438,17 +461,37 @@ __device__ __forceinline__ void move_typed(const ListParams &P, const Piece &p, 
     }
 }
 
+// What can be loaded of an item's products before the norm is known (Adam step: the lanes' first units).
 template <ClipKind K>
-__device__ __forceinline__ void products(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t worker, AdamStep &k, float lr,
-                                         uint32_t lane, uint32_t held)
+struct Early {};
+template <>
+struct Early<kAdam> { AdamPlace place; AdamUnit first; float decay; };
+template <>
+struct Early<kAdamMaster> : Early<kAdam> {};
+
+template <ClipKind K>
+__device__ __forceinline__ Early<K> load_early(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t lane, uint32_t held)
+{
+    Early<K> r{};
+    if constexpr (is_adam(K)) {
+        r.place = adam_place<K == kAdamMaster>(P.adam, p, base.tensor);
+        if (lane < r.place.units) r.first = adam_load<K == kAdamMaster>(r.place, lane, held, lane);
+        if (P.adam.decay != nullptr) r.decay = ld_global(P.adam.decay + p.tensor);
+    }
+    return r;
+}
+
+template <ClipKind K>
+__device__ __forceinline__ void products(const ListParams &P, const Piece &p, const ItemBase &base, const Early<K> &early, uint32_t worker, AdamStep &k,
+                                         float lr, uint32_t lane, uint32_t held)
 {
     const uint32_t type = p.len_type >> 16;
-    if constexpr (K == kAdam || K == kAdamMaster) {
-        const double wd = P.adam.decay != nullptr ? (double)ld_global(P.adam.decay + p.tensor) : P.adam.weight_decay;
-        k.keep = (float)(1.0 - (double)lr * wd);
-        if (K == kAdam || type == THC_F32) adam_piece<THC_F32, K == kAdamMaster>(P.adam, k, p, base.tensor, lane, held);
-        else if (type == THC_BF16) adam_piece<THC_BF16, K == kAdamMaster>(P.adam, k, p, base.tensor, lane, held);
-        else adam_piece<THC_F16, K == kAdamMaster>(P.adam, k, p, base.tensor, lane, held);
+    if constexpr (is_adam(K)) {
+        constexpr bool kMaster = K == kAdamMaster;
+        k.keep = (float)(1.0 - (double)lr * (P.adam.decay != nullptr ? (double)early.decay : P.adam.weight_decay));
+        if (!kMaster || type == THC_F32) adam_item<THC_F32, kMaster>(early.place, k, early.first, lane, held);
+        else if (type == THC_BF16) adam_item<THC_BF16, kMaster>(early.place, k, early.first, lane, held);
+        else adam_item<THC_F16, kMaster>(early.place, k, early.first, lane, held);
     } else {
         if (type == THC_F32) move_typed<K, THC_F32>(P, p, base, worker, k.c, lane, held);
         else if (type == THC_BF16) move_typed<K, THC_BF16>(P, p, base, worker, k.c, lane, held);
@@ -465,12 +508,19 @@ __device__ __forceinline__ void adam_constants(const AdamParams &a, AdamStep &k)
     k.a2 = (float)(1.0 - a.beta2);
     k.eps = (float)a.eps;
 }
-// Those that depend on the step count t (in the norm's result: step_size, inv_sqrt_by2).
-__device__ __forceinline__ void adam_sizes(const AdamParams &a, float lr, int64_t t, float *step_size, float *inv_sqrt_by2)
+// beta^t by squaring.  Each product's rounding counts t times at most: t beta^t 2^-53 <= 2^-53 / (e (1 - beta)) off.  (pow() was
+// a third of a small step's time.)
+__device__ __forceinline__ double power(double beta, uint64_t t)
 {
-    *step_size = (float)((double)lr / (1.0 - pow(a.beta1, (double)t)));
-    *inv_sqrt_by2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
+    double r = 1.0;
+#pragma unroll 1
+    for (; t != 0u; t >>= 1, beta *= beta)
+        if (t & 1u) r *= beta;
+    return r;
 }
+// Those that depend on the step count t (in the norm's result: step_size, inv_sqrt_by2).
+__device__ __forceinline__ float adam_step_size(const AdamParams &a, float lr, int64_t t) { return (float)((double)lr / (1.0 - power(a.beta1, (uint64_t)t))); }
+__device__ __forceinline__ float adam_inv_sqrt(const AdamParams &a, int64_t t) { return (float)(1.0 / sqrt(1.0 - power(a.beta2, (uint64_t)t))); }
 
 // Norm to the caller, factor to the products.  ADAM: also the step count, unless the norm is not finite.
 template <bool ADAM>
@@ -486,7 +536,8 @@ __device__ __forceinline__ NormResult finish_norm(const ListParams &P, uint32_t 
     } else if (ADAM) {
         const int64_t t = *P.adam.step + 1;
         *P.adam.step = t;
-        adam_sizes(P.adam, *P.adam.lr, t, &r.step_size, &r.inv_sqrt_by2);
+        r.step_size = adam_step_size(P.adam, *P.adam.lr, t);
+        r.inv_sqrt_by2 = adam_inv_sqrt(P.adam, t);
     }
     return r;
 }
@@ -534,7 +585,7 @@ list_norm_kernel(const __grid_constant__ ListParams P)
 
 // Products of eight items to a CTA, over all workers; the last ones first.
 template <ClipKind K>
-__global__ void __launch_bounds__(kListThreads, kProductCtasPerSm)
+__global__ void __launch_bounds__(kListThreads, product_ctas_per_sm(K))
 list_product_kernel(const __grid_constant__ ListParams P)
 {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -547,18 +598,22 @@ list_product_kernel(const __grid_constant__ ListParams P)
     AdamStep k{};
     k.c = Factor{1.0f, 1.0f};
     float lr = 0.0f;
+    uint4 q{};
+    uint32_t stop = 0u;
     if (P.norms != nullptr) {
-        const uint4 q = ld_global(reinterpret_cast<const uint4 *>(P.result + worker));
-        k.c = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
-        if (is_adam(K)) {
-            if (ld_global(&P.result->stop) != 0u) return;   // the norm is not finite
-            k.step_size = __uint_as_float(q.z);
-            k.inv_sqrt_by2 = __uint_as_float(q.w);
-            lr = ld_global(P.adam.lr);
-            adam_constants(P.adam, k);
-        }
+        q = ld_global(reinterpret_cast<const uint4 *>(P.result + worker));
+        if (is_adam(K)) stop = ld_global(&P.result[worker].stop);
     }
-    products<K>(P, p, base, worker, k, lr, lane, kNotHeld);
+    if (is_adam(K)) lr = ld_global(P.adam.lr);
+    const Early<K> early = load_early<K>(P, p, base, lane, kNotHeld);
+    if (P.norms != nullptr) {
+        if (is_adam(K) && stop != 0u) return;          // the norm is not finite
+        k.c = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
+        k.step_size = __uint_as_float(q.z);
+        k.inv_sqrt_by2 = __uint_as_float(q.w);
+    }
+    if (is_adam(K)) adam_constants(P.adam, k);
+    products<K>(P, p, base, early, worker, k, lr, lane, kNotHeld);
 }
 
 // Both in one launch, grid (8 CTAs, workers), a cluster per worker.  The CTAs' sums are written to all CTAs' shared memory;
@@ -587,6 +642,9 @@ list_cluster_kernel(const __grid_constant__ ListParams P)
         lr = ld_global(P.adam.lr);
         t = (int64_t)load_base(reinterpret_cast<const uint64_t *>(P.adam.step)) + 1;
     }
+    // by the CTA's last warps, which have no item in the shortest lists
+    if (is_adam(K) && threadIdx.x == kClusterThreads - 32) s_result.step_size = adam_step_size(P.adam, lr, t);
+    if (is_adam(K) && threadIdx.x == kClusterThreads - 64) s_result.inv_sqrt_by2 = adam_inv_sqrt(P.adam, t);
     double s = 0.0;
 #pragma unroll 1
     for (; c < items; c += stride) {
@@ -595,6 +653,8 @@ list_cluster_kernel(const __grid_constant__ ListParams P)
         else last_base = load_item_base<K>(P, last, worker);
         s += squares<true>(last, base, P.src_flat, lane, c + stride < items ? kNotHeld : held);
     }
+    Early<K> early{};
+    if (first < items) early = load_early<K>(P, last, last_base, lane, held);
     const double sum = sum_of_cta(s, red);
     if (threadIdx.x == 0) {
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x]);
@@ -603,7 +663,6 @@ list_cluster_kernel(const __grid_constant__ ListParams P)
             asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f64 [a], %2;\n\t}" :: "r"(to), "r"(r), "d"(sum) : "memory");
     }
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    if (is_adam(K) && threadIdx.x == 0) adam_sizes(P.adam, lr, t, &s_result.step_size, &s_result.inv_sqrt_by2);
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x == 0) {
         double total = 0.0;
@@ -627,12 +686,13 @@ list_cluster_kernel(const __grid_constant__ ListParams P)
     k.c = s_result.c;
     if (first >= items) return;
     const uint32_t final = first + (items - 1u - first) / stride * stride;
-    products<K>(P, last, last_base, worker, k, lr, lane, held);
+    products<K>(P, last, last_base, early, worker, k, lr, lane, held);
 #pragma unroll 1
     for (c = final; c >= stride; ) {
         c -= stride;
         p = load_item(P.L, c, P.split_log2);
-        products<K>(P, p, load_item_base<K>(P, p, worker), worker, k, lr, lane, kNotHeld);
+        last_base = load_item_base<K>(P, p, worker);
+        products<K>(P, p, last_base, load_early<K>(P, p, last_base, lane, kNotHeld), worker, k, lr, lane, kNotHeld);
     }
 }
 
@@ -920,7 +980,7 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
 }
 
 // Lists of at most this many pieces a worker take the cluster.
-constexpr uint32_t kClusterMostPieces = 256;
+constexpr uint32_t kClusterMostPieces = 64;
 
 template <ClipKind K>
 static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace, void *stream)
@@ -953,7 +1013,7 @@ static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, 
         const int rc = launch_norm(P, h, list_norm_kernel<is_adam(K)>, st);
         if (rc != THC_OK) return rc;
     }
-    P.split_log2 = split_of(h, (uint64_t)h->sm_count * kProductCtasPerSm * kListWarps / h->n);
+    P.split_log2 = split_of(h, (uint64_t)h->sm_count * product_ctas_per_sm(K) * kListWarps / h->n);
     const uint64_t items = ((uint64_t)h->pieces_n << P.split_log2) * h->n;
     THC_CUDA(launch_after(list_product_kernel<K>, dim3((unsigned)((items + kListWarps - 1) / kListWarps)), kListThreads, 0, st, P));
     return THC_OK;
