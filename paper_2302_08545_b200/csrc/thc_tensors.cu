@@ -169,6 +169,31 @@ __device__ __forceinline__ Raw<T> held_unit(uint32_t held, uint32_t b, uint32_t 
 constexpr uint32_t kNotHeld = 0xFFFFFFFFu;
 
 // ---------------------------------------------------------------------------------- norm
+// s + the squares of a unit.  fp32: each square in fp64, which no value leaves.  16 bits: the squares are exact in fp32, eight
+// of them are added there in three levels (3 x 2^-24 off at most, as all are positive) and the sum in fp64: a conversion and an fp64
+// operation per unit instead of eight, which were what bounded it (355M bf16: 125 us, now 111).  fp16's squares and their sums
+// stay within fp32; for bf16 a sum outside [2^-100, 2^126] (a square may have left fp32's range) is formed as for fp32.
+template <uint32_t T>
+__device__ __forceinline__ void add_squares(double (&s)[2], const Raw<T> &r)
+{
+    if constexpr (T != THC_F32) {
+        float q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = fmaf(value<T>(r, 2 * i), value<T>(r, 2 * i), value<T>(r, 2 * i + 1) * value<T>(r, 2 * i + 1));
+        const float sum = (q[0] + q[1]) + (q[2] + q[3]);
+        if (T == THC_F16 || (sum >= 0x1p-100f && sum <= 0x1p126f)) {
+            s[0] += (double)sum;
+            return;
+        }
+        if (((r.w[0] | r.w[1] | r.w[2] | r.w[3]) & 0x7FFF7FFFu) == 0u) return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const double v = (double)value<T>(r, e);
+        s[e & 1] = fma(v, v, s[e & 1]);
+    }
+}
+
 // Sum of squares of a piece, in a lane; its units go to `held` unless that is kNotHeld.
 template <uint32_t T, bool HOLD>
 __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uint32_t lane, uint32_t held)
@@ -193,11 +218,7 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
         for (int b = 0; b < kBatch; ++b) {
             if (HOLD && held != kNotHeld) hold_unit<T>(held, first + b, lane, r[b]);
             if (!kWhole && lane + 32u * b >= left) r[b] = Raw<T>{};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double v = (double)value<T>(r[b], e);
-                s[e & 1] = fma(v, v, s[e & 1]);
-            }
+            add_squares<T>(s, r[b]);
         }
         at += 32u * kBatch * kUnit * size_of<T>();
         first += kBatch;
@@ -210,13 +231,14 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
     return fma(v, v, s[0]) + s[1];
 }
 
-template <bool HOLD>
+// ONLY32: nothing but fp32 is read.
+template <bool HOLD, bool ONLY32 = false>
 __device__ __forceinline__ double squares(const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane, uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu, type = p.len_type >> 16;
     if (flat != 0) return squares_of_piece<THC_F32, HOLD>(flat + p.flat * 4u, len, lane, held);
     const uint64_t b = load_base(base + p.tensor);
-    if (type == THC_F32) return squares_of_piece<THC_F32, HOLD>(b + p.flat * 4u, len, lane, held);
+    if (ONLY32 || type == THC_F32) return squares_of_piece<THC_F32, HOLD>(b + p.flat * 4u, len, lane, held);
     if (type == THC_BF16) return squares_of_piece<THC_BF16, HOLD>(b + p.flat * 2u, len, lane, held);
     return squares_of_piece<THC_F16, HOLD>(b + p.flat * 2u, len, lane, held);
 }
@@ -522,29 +544,11 @@ __device__ __forceinline__ double power(double beta, uint64_t t)
 __device__ __forceinline__ float adam_step_size(const AdamParams &a, float lr, int64_t t) { return (float)((double)lr / (1.0 - power(a.beta1, (uint64_t)t))); }
 __device__ __forceinline__ float adam_inv_sqrt(const AdamParams &a, int64_t t) { return (float)(1.0 / sqrt(1.0 - power(a.beta2, (uint64_t)t))); }
 
-// Norm to the caller, factor to the products.  ADAM: also the step count, unless the norm is not finite.
-template <bool ADAM>
-__device__ __forceinline__ NormResult finish_norm(const ListParams &P, uint32_t worker, double sum)
-{
-    const double norm = sqrt(sum);
-    NormResult r{};
-    r.c = factor_of(norm, P.max_norm);
-    P.norms[worker] = (float)norm;
-    if (!isfinite(norm)) {
-        atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
-        r.stop = 1u;
-    } else if (ADAM) {
-        const int64_t t = *P.adam.step + 1;
-        *P.adam.step = t;
-        r.step_size = adam_step_size(P.adam, *P.adam.lr, t);
-        r.inv_sqrt_by2 = adam_inv_sqrt(P.adam, t);
-    }
-    return r;
-}
-
 // Sums of squares, grid (CTAs of a worker, workers).  A warp's pieces are fixed by the grid and the sums are added in a fixed
-// order; a worker's last CTA does that.
-template <bool ADAM>
+// order; a worker's last CTA does that and forms what the products need (ADAM: also the step count, unless the norm is not
+// finite).  ONLY32: the same with nothing but fp32 to read (with the code for 16 bits beside it the registers do not suffice, and
+// eight workers' 25.6M fp32 take 135 us instead of 117).
+template <bool ADAM, bool ONLY32>
 __global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
 list_norm_kernel(const __grid_constant__ ListParams P)
 {
@@ -561,26 +565,37 @@ list_norm_kernel(const __grid_constant__ ListParams P)
         const Piece now = p;
         c += stride;
         if (c < items) p = load_item(P.L, c, P.split_log2);
-        s += squares<false>(now, base, P.src_flat, lane, kNotHeld);
+        s += squares<false, ONLY32>(now, base, P.src_flat, lane, kNotHeld);
     }
     __shared__ double red[kListWarps];
+    __shared__ NormResult s_result;
     __shared__ uint32_t last;
-    double t = sum_of_cta(s, red);
+    double sum = sum_of_cta(s, red);
     if (threadIdx.x == 0) {
-        __stcg(P.partial + (uint64_t)worker * gridDim.x + blockIdx.x, t);
+        __stcg(P.partial + (uint64_t)worker * gridDim.x + blockIdx.x, sum);
         __threadfence();
         last = atomicInc(P.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
-    t = 0.0;
-    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) t += __ldcg(P.partial + (uint64_t)worker * gridDim.x + i);
-    t = sum_of_cta(t, red);
-    if (threadIdx.x == 0) {
-        const NormResult r = finish_norm<ADAM>(P, worker, t);
-        if (P.result != nullptr) P.result[worker] = r;
+    int64_t t = 0;
+    if (ADAM && (lane == 0u) && warp < 3u) {           // three threads of three warps at a time
+        t = (int64_t)load_base(reinterpret_cast<const uint64_t *>(P.adam.step)) + 1;
+        if (warp == 1u) s_result.step_size = adam_step_size(P.adam, ld_global(P.adam.lr), t);
+        if (warp == 2u) s_result.inv_sqrt_by2 = adam_inv_sqrt(P.adam, t);
     }
+    sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(P.partial + (uint64_t)worker * gridDim.x + i);
+    sum = sum_of_cta(sum, red);                        // (with a barrier: the two sizes are there)
+    if (threadIdx.x != 0) return;
+    const double norm = sqrt(sum);
+    P.norms[worker] = (float)norm;
+    s_result.c = factor_of(norm, P.max_norm);
+    s_result.stop = isfinite(norm) ? 0u : 1u;
+    if (!isfinite(norm)) atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
+    else if (ADAM) *P.adam.step = t;
+    if (P.result != nullptr) P.result[worker] = s_result;
 }
 
 // Products of eight items to a CTA, over all workers; the last ones first.
@@ -959,10 +974,13 @@ static void fill_params(ListParams &P, const thc_ctx *ctx, const thc_tensors *h,
     P.dev = view_of(ctx).dev;
 }
 
-static int launch_norm(ListParams &P, const thc_tensors *h, void (*kern)(ListParams), cudaStream_t st)
+template <bool ADAM>
+static int launch_norm(ListParams &P, const thc_tensors *h, cudaStream_t st)
 {
     P.split_log2 = split_of(h, (uint64_t)h->sm_count * kListWarps / h->n);
-    THC_CUDA(launch_after(kern, dim3(norm_ctas(h, P.split_log2), h->n), kListThreads, 0, st, P));
+    const dim3 grid(norm_ctas(h, P.split_log2), h->n);
+    if (ADAM || P.src_flat != 0 || h->all_f32) THC_CUDA(launch_after(list_norm_kernel<ADAM, true>, grid, kListThreads, 0, st, P));
+    else THC_CUDA(launch_after(list_norm_kernel<false, false>, grid, kListThreads, 0, st, P));
     return THC_OK;
 }
 
@@ -976,18 +994,21 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
     memset(&P, 0, sizeof P);
     fill_params(P, ctx, list, INFINITY, norms, workspace);
     P.result = nullptr;
-    return launch_norm(P, list, list_norm_kernel<false>, static_cast<cudaStream_t>(stream));
+    return launch_norm<false>(P, list, static_cast<cudaStream_t>(stream));
 }
 
-// Lists of at most this many pieces a worker take the cluster.
-constexpr uint32_t kClusterMostPieces = 64;
+// Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
+//   pieces          16          32          48          64          96
+//   gather       4.3 / 6.9   4.5 / 7.0   5.2 / 7.0   5.2 / 6.9   8.2 / 6.9
+//   Adam step    6.2 / 8.7   7.9 / 8.6  10.2 / 8.5  10.4 / 8.4  17.9 / 8.3
+static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 32u : 64u; }
 
 template <ClipKind K>
 static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace, void *stream)
 {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     fill_params(P, ctx, h, max_norm, norms, workspace);
-    if (norms != nullptr && h->pieces_n <= kClusterMostPieces) {
+    if (norms != nullptr && h->pieces_n <= cluster_most_pieces(K)) {
         P.split_log2 = std::max(1u, split_of(h, kClusterCtas * kClusterWarps));   // (1: see kHeldBytes)
         const void *kern = reinterpret_cast<const void *>(list_cluster_kernel<K>);
         const int rc = ensure_dynamic_smem(kern);
@@ -1010,7 +1031,7 @@ static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, 
         return THC_OK;
     }
     if (norms != nullptr) {
-        const int rc = launch_norm(P, h, list_norm_kernel<is_adam(K)>, st);
+        const int rc = launch_norm<is_adam(K)>(P, h, st);
         if (rc != THC_OK) return rc;
     }
     P.split_log2 = split_of(h, (uint64_t)h->sm_count * product_ctas_per_sm(K) * kListWarps / h->n);

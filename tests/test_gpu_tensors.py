@@ -1,15 +1,18 @@
 """Lists of tensors on the GPU: norm, clipping, the ways into and out of the flat vector and the Adam step against
 their definitions in 64 bits.
 
-Bounds: the norm is an fp64 sum rounded to fp32 (one rounding, u = 2^-24); the factor is formed in fp64 and rounded
-(u), the product is rounded (u), then once more to the tensor's type.  The Adam step's are beside its test."""
+Bounds, with u = 2^-24: fp32 squares are added in fp64.  Eight exact squares of 16-bit values are added in fp32 in three
+levels, each of which is off by at most u of a sum of positive terms, 3 u in all, and then in fp64; the norm, a square root, is
+off by half of that, before(list) = 1.5 u, or 0 without 16-bit tensors.  It is rounded to fp32 (u).  The factor is formed in fp64
+from the norm before that rounding, so it is off by before(list), and rounded (u); the product is rounded (u), then once more to
+the tensor's type.  The Adam step's bounds are beside its test."""
 import math
 
 import pytest
 import torch
 
 import tensor_lists as T
-from tensor_lists import U
+from tensor_lists import TYPES, U
 
 pytestmark = pytest.mark.gpu
 
@@ -32,9 +35,13 @@ def setup(workers, in_dtype="f32"):
     return ctx, lst, norms, ws
 
 
+def before(workers):
+    return 0.0 if all(x.dtype == torch.float32 for x in workers[0]) else 1.5 * U
+
+
 def check_norms(norms, workers):
     ref = torch.tensor([T.norm(w) for w in workers], dtype=torch.float64)
-    T.within(norms.cpu(), ref, ref * U * SMALL)
+    T.within(norms.cpu(), ref, ref * (before(workers) + U) * SMALL)
     return ref.tolist()
 
 
@@ -63,20 +70,20 @@ def test_norm(sizes, types, n, shift):
 def test_clip(sizes, types, n, shift, in_place):
     from paper_2302_08545_b200 import thc
     workers = T.make(sizes, types, n, shift, seed=3)
-    before = [[x.clone() for x in w] for w in workers]
+    old = [[x.clone() for x in w] for w in workers]
     ctx, lst, norms, ws = setup(workers)
     most = 0.7 * T.norm(workers[0])        # clips some workers or all
     outs = workers if in_place else T.make(sizes, types, n, shift + 1 if shift else 0, seed=9)
     ctx.clip_grads(lst, most, norms, ws, out=None if in_place else thc.Tensors(ctx, outs))
-    ref = check_norms(norms, before)
-    for w, o, r in zip(before, outs, ref):
+    ref = check_norms(norms, old)
+    for w, o, r in zip(old, outs, ref):
         c = T.factor(r, most)
         for x, y in zip(w, o):
             exact = x.double() * c
             rel, least = T.half_step(y.dtype)
-            T.within(y, exact, exact.abs() * ((2 * U + (rel if y.dtype != torch.float32 else 0)) * SMALL) + least + 2.0 ** -149)
+            T.within(y, exact, exact.abs() * ((before(old) + 2 * U + (rel if y.dtype != torch.float32 else 0)) * SMALL) + least + 2.0 ** -149)
     if not in_place:
-        for w, b in zip(workers, before):
+        for w, b in zip(workers, old):
             assert all(torch.equal(x, y) for x, y in zip(w, b))
 
 
@@ -97,11 +104,11 @@ def test_clip_leaves_what_is_around_the_tensors_alone():
 @pytest.mark.parametrize("below", [True, False])
 def test_a_norm_below_the_bound_changes_nothing(below):
     workers = T.make(EDGES, ["f32", "bf16", "f16"], 2, seed=4)
-    before = [[x.clone() for x in w] for w in workers]
+    old = [[x.clone() for x in w] for w in workers]
     ctx, lst, norms, ws = setup(workers)
     ctx.clip_grads(lst, 1e9 if below else math.inf, norms, ws)
-    assert all(torch.equal(x, y) for w, b in zip(workers, before) for x, y in zip(w, b))
-    check_norms(norms, before)
+    assert all(torch.equal(x, y) for w, b in zip(workers, old) for x, y in zip(w, b))
+    check_norms(norms, old)
 
 
 def test_max_norm_zero_and_zero_gradients():
@@ -118,13 +125,13 @@ def test_values_that_are_not_finite(value):
     from paper_2302_08545_b200 import thc
     workers = T.make([100, 5000], ["f32", "bf16"], 3, seed=4)
     workers[1][1][4321] = value
-    before = [[x.clone() for x in w] for w in workers]
+    old = [[x.clone() for x in w] for w in workers]
     ctx, lst, norms, ws = setup(workers)
     ctx.clip_grads(lst, 1.0, norms, ws)
     assert ctx.status() == thc.STATUS_NONFINITE and ctx.status() == 0
     got = norms.tolist()
     assert math.isfinite(got[0]) and math.isfinite(got[2]) and (math.isnan(got[1]) if math.isnan(value) else got[1] == math.inf)
-    for x, y in zip(workers[1], before[1]):
+    for x, y in zip(workers[1], old[1]):
         if math.isnan(value):
             assert bool(torch.isnan(x).all())
         else:
@@ -145,6 +152,24 @@ def test_values_whose_squares_leave_fp32():
     assert math.isinf(float(norms)) and ctx.status() == 0      # past fp32, not past fp64
     exact = y.double() * (2.0 / (math.sqrt(5000) * float(y[0].double()) + 1e-6))
     T.within(x, exact, exact.abs() * 2 * U * SMALL)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_squares_of_16_bits_at_the_ends_of_their_range(dtype):
+    """Units whose squares leave fp32's range, next to ordinary ones, zeros and denormals; and all of one kind."""
+    values = [3e38, 1e30, 1e-30, 1e-38, 1e-40, 0.0, 1.0, -2e19, 5e-20] if dtype == "bf16" else [65504.0, 6e-8, 6.1e-5, 0.0, 1.0, -3e-6]
+    rows = [[v] * 8 for v in values] + [[v] * 3 + [values[0]] + [0.0] * 4 for v in values] + [[0.0] * 7 + [v] for v in values]
+    for chosen in [rows, rows[1:], rows[2:5] * 9, rows[3:6] * 9] + [[r] * 40 for r in rows]:
+        x = torch.tensor(chosen, dtype=torch.float64, device="cuda").to(TYPES[dtype]).reshape(-1)
+        for pieces in ([x], [x, torch.zeros(5000, dtype=x.dtype, device="cuda")]):
+            ctx, lst, norms, ws = setup([pieces])
+            ctx.grad_norm(lst, norms, ws)
+            ref = T.norm(pieces)
+            if ref > 3.4e38:
+                assert math.isinf(float(norms))
+            else:
+                T.within(norms.cpu(), torch.tensor([ref], dtype=torch.float64), torch.tensor([ref * 2.5 * U * SMALL + 2.0 ** -150], dtype=torch.float64))
+            assert ctx.status() == 0
 
 
 @pytest.mark.parametrize("flat", ["f32", "bf16", "residual", "residual in place"])
@@ -171,8 +196,8 @@ def test_gather(sizes, types, n, shift, flat):
             v.copy_(x.double() * c)
         exact += product
         rel = T.half_step(dt)[0]
-        # factor: u of the product; one rounding of the result (fp32: of the product or of the fused sum)
-        bound = product.abs() * U + exact.abs() * (U + (rel if flat == "bf16" else 0))
+        # factor: before(list) + u of the product; one rounding of the result (fp32: of the product or of the fused sum)
+        bound = product.abs() * (before(workers) + U) + exact.abs() * (U + (rel if flat == "bf16" else 0))
         T.within(y, exact, bound * SMALL + 2.0 ** -149)
         T.within(y[product == 0], e[product == 0], torch.zeros_like(e[product == 0]))
     assert bool((room[:, lst.d:] == 7.0).all())
@@ -199,7 +224,7 @@ def test_scatter(sizes, types, n, shift):
     workers = T.make(sizes, types, 1, shift, seed=6)
     ctx, lst, norms, ws = setup(workers)
     flat = torch.randn(lst.d, device="cuda")
-    before = flat.clone()
+    old = flat.clone()
     views = lst.views(flat)
     most = 0.5 * T.norm(views)
     ctx.scatter_grads(flat, most, lst, norms, ws)
@@ -208,7 +233,7 @@ def test_scatter(sizes, types, n, shift):
         exact = v.double() * T.factor(r, most)
         rel, least = T.half_step(x.dtype)
         T.within(x, exact, exact.abs() * ((2 * U + (rel if x.dtype != torch.float32 else 0)) * SMALL) + least + 2.0 ** -149)
-    assert torch.equal(flat, before)
+    assert torch.equal(flat, old)
     ctx.scatter_grads(flat, math.inf, lst, None, None)
     assert all(torch.equal(x, v.to(x.dtype)) for x, v in zip(workers[0], views))
 
@@ -218,11 +243,11 @@ def test_scatter_to_places_in_the_flat_vector_itself():
     sizes = [100, 5000, 63]
     ctx, lst, norms, ws = setup(T.make(sizes, ["f32"], 1))
     flat = torch.randn(lst.d, device="cuda")
-    before = flat.clone()
+    old = flat.clone()
     own = thc.Tensors(ctx, [lst.views(flat)])
     ctx.scatter_grads(flat, 1.0, own, norms, ws)
-    r, = check_norms(norms, [lst.views(before)])
-    exact = before.double()
+    r, = check_norms(norms, [lst.views(old)])
+    exact = old.double()
     for v in lst.views(exact):
         v.mul_(T.factor(r, 1.0))
     T.within(flat, exact, exact.abs() * 2 * U * SMALL)
@@ -270,13 +295,13 @@ def test_adamw(sizes, types, shift, master, per_tensor):
     for t in (5, 6, 7):
         old = [x.clone() for x in (m, v)] + ([wm.clone()] if master else [])
         weights = [x.double() for x in (lst.views(wm) if master else workers[0])]
-        before = [x.double() for x in (grad, m, v)]
+        wide = [x.double() for x in (grad, m, v)]
         most = 0.5 * T.norm(lst.views(grad)) if t < 7 else math.inf
         ctx.adamw(grad, lst, lr, step, m, v, norms, ws, master=wm, decay=decay, betas=(b1, b2), eps=eps, weight_decay=0.05, max_norm=most)
         assert int(step) == t
         r, = check_norms(norms, [lst.views(grad)])
         for i, x in enumerate(workers[0]):
-            g0, m0, v0 = (lst.views(y)[i] for y in before)
+            g0, m0, v0 = (lst.views(y)[i] for y in wide)
             wd = float(decay[i]) if per_tensor else 0.05
             m2, v2, w2, dm, dv, dw = adam_exact(g0, m0, v0, weights[i], T.factor(r, most), t, float(lr), wd, b1, b2, eps)
             T.within(lst.views(m)[i], m2, dm)
