@@ -26,13 +26,21 @@ plain loads only), and q stores its sums into every rank's buffer.  Two stream-o
 per round (a one-element all-reduce each) replace the all-to-all and the all-gather; no kernel
 ever waits on another rank.
 
+step_tensors is a round that begins with a program's many gradient tensors (thc.Tensors), clipped by the rank's norm, and
+keeps the residual of error feedback; CudaOps.scatter and CudaOps.adamw lead from its average back to tensors.  Every rank has
+the same average, so every rank clips it by the same norm and takes the same step.
+
 The exchange logic takes the per-rank steps as an `ops` object, so that it can be exercised on
 CPU process groups; the only implementation in this package, CudaOps, calls the library.
 """
 from __future__ import annotations
 
+import math
+
 import torch
 import torch.distributed as dist
+
+from . import thc
 
 
 def block_ranges(nblocks: int, world: int):
@@ -59,7 +67,10 @@ class CudaOps:
         self.scales = torch.empty(self.sz.nblocks, dtype=torch.float32, device=device)
         self.packed = torch.empty(self.sz.packed_bytes, **u8)
         self.out = torch.empty(d, dtype=torch.float32, device=device)
+        self.norm = torch.zeros(1, dtype=torch.float32, device=device)       # of the rank's own gradients
+        self.average_norm = torch.zeros(1, dtype=torch.float32, device=device)
         self._part = {}
+        self._flat = self._list_workspace = None
 
     def local_scales(self, grad):
         self.ctx.prepare([grad], self.d, self.scales, self.workspace)
@@ -86,6 +97,34 @@ class CudaOps:
     def decompress(self, total, divisor: int, rnd: int, scales):
         self.ctx.decompress(total, divisor, self.d, rnd, scales, self.out, self.workspace)
         return self.out
+
+    # -- between the round and a program's tensors (thc.Tensors with one worker and d = the round's)
+    def _workspace_of(self, tensors):
+        if tensors.d != self.d or tensors.n != 1:
+            raise ValueError(f"a list of one worker whose flat vector has {self.d} elements is expected")
+        if self._list_workspace is None or self._list_workspace.nbytes < tensors.workspace_bytes:
+            self._list_workspace = torch.empty(tensors.workspace_bytes, dtype=torch.uint8, device=self.device)
+        return self._list_workspace
+
+    def gather(self, tensors, max_norm: float = math.inf, ef=None):
+        """The rank's gradients, clipped by their norm, as the vector that is compressed; plus the residual ef."""
+        workspace = self._workspace_of(tensors)
+        if self._flat is None:
+            kind = torch.bfloat16 if self.ctx.in_dtype == thc.THC_BF16 else torch.float32
+            self._flat = torch.empty(self.d, dtype=kind, device=self.device)
+        self.ctx.gather_grads(tensors, max_norm, [self._flat], self.norm, workspace, ef=None if ef is None else [ef])
+        return self._flat
+
+    def residual(self, grad, packed, rnd: int, scales, ef):
+        self.ctx.error_feedback([grad], [packed], self.d, rnd, scales, [ef], self.workspace)
+
+    def scatter(self, out, tensors, max_norm: float = math.inf):
+        """The average, clipped by its norm, to tensors."""
+        self.ctx.scatter_grads(out, max_norm, tensors, self.average_norm, self._workspace_of(tensors))
+
+    def adamw(self, out, tensors, lr, step, m, v, master=None, **how):
+        """An Adam step of the weights with the average (arguments as thc.Context.adamw)."""
+        self.ctx.adamw(out, tensors, lr, step, m, v, self.average_norm, self._workspace_of(tensors), master=master, **how)
 
 
 class DataParallelRound:
@@ -162,6 +201,15 @@ class DataParallelRound:
                 at += n
         # 6. estimate + inverse RHT with divisor n
         out = ops.decompress(total, world, rnd, scales)
+        return out, scales, packed, total
+
+    def step_tensors(self, tensors, rnd: int, max_norm: float = math.inf, ef=None):
+        """step() with the rank's gradient tensors, clipped by their norm.  ef (fp32, the flat vector's length): the
+        residual of the rank's previous round, which is added, and replaced by this round's."""
+        grad = self.ops.gather(tensors, max_norm, ef)
+        out, scales, packed, total = self.step(grad, rnd)
+        if ef is not None:
+            self.ops.residual(grad, packed, rnd, scales, ef)
         return out, scales, packed, total
 
 

@@ -2,6 +2,8 @@
 and issue prepare / compress / aggregate / decompress in order.  No arithmetic here."""
 from __future__ import annotations
 
+import math
+
 import numpy as np
 import torch
 
@@ -93,3 +95,46 @@ class Round:
         else:
             self.aggregate(stream)
             self.decompress(rnd, stream)
+
+
+class TensorRound:
+    """A round between a program's tensors, n workers' lists of them on one GPU: the gradients, clipped by each
+    worker's norm, become the flat vectors that the round compresses; its average goes, clipped again, back to
+    tensors (scatter) or through an Adam step into the weights (adamw).
+
+    ``grads`` is a sequence of n sequences of tensors (see thc.Tensors).  With error feedback each worker's
+    residual of one round is added to its gradients of the next (fp32 contexts)."""
+
+    def __init__(self, ctx: thc.Context, grads, error_feedback: bool = False):
+        self.ctx = ctx
+        self.grads = thc.Tensors(ctx, grads)
+        n, d, device = self.grads.n, self.grads.d, grads[0][0].device
+        self.round = Round(ctx, n, d, "bf16" if ctx.in_dtype == thc.THC_BF16 else "f32", device=device)
+        self.norms = torch.zeros(n, dtype=torch.float32, device=device)
+        self.average_norm = torch.zeros(1, dtype=torch.float32, device=device)
+        self.workspace = None
+        self._workspace_of(self.grads)
+        self.ef = [torch.zeros(d, dtype=torch.float32, device=device) for _ in range(n)] if error_feedback else None
+
+    def _workspace_of(self, tensors: thc.Tensors):
+        if self.workspace is None or self.workspace.nbytes < tensors.workspace_bytes:
+            self.workspace = torch.empty(tensors.workspace_bytes, dtype=torch.uint8, device=self.round.device)
+        return self.workspace
+
+    def run(self, rnd: int = 0, max_norm: float = math.inf, stream=None):
+        """Gather and the round; returns the flat average (a buffer of this object)."""
+        r = self.round
+        self.ctx.gather_grads(self.grads, max_norm, r.grads, self.norms, self.workspace, ef=self.ef, stream=stream)
+        r.run(rnd, fused=True, stream=stream)
+        if self.ef is not None:
+            self.ctx.error_feedback(r.grads, r.packed, r.d, rnd, r.scales, self.ef, r.workspace, stream)
+        return r.out
+
+    def scatter(self, tensors: thc.Tensors, max_norm: float = math.inf, stream=None):
+        """The average, clipped by its norm, to the tensors of a list with one worker."""
+        self.ctx.scatter_grads(self.round.out, max_norm, tensors, self.average_norm, self._workspace_of(tensors), stream)
+
+    def adamw(self, weights: thc.Tensors, lr, step, m, v, master=None, stream=None, **how):
+        """An Adam step with the average (arguments as thc.Context.adamw)."""
+        self.ctx.adamw(self.round.out, weights, lr, step, m, v, self.average_norm, self._workspace_of(weights),
+                       master=master, stream=stream, **how)
