@@ -440,6 +440,7 @@ struct ListParams {
     double max_norm;
     float *norms;                // or null: no norm, factor 1
     double *partial;             // workspace: a sum per CTA
+    uint32_t partials;           // sums per worker that list_product_kernel adds itself, or 0: it finds the result
     NormResult *result;          // workspace: one per worker
     DeviceBlock *dev;
     AdamParams adam;
@@ -546,8 +547,8 @@ __device__ __forceinline__ float adam_inv_sqrt(const AdamParams &a, int64_t t) {
 
 // Sums of squares, grid (CTAs of a worker, workers).  A warp's pieces are fixed by the grid and the sums are added in a fixed
 // order; a worker's last CTA does that and forms what the products need (ADAM: also the step count, unless the norm is not
-// finite).  ONLY32: the same with nothing but fp32 to read (with the code for 16 bits beside it the registers do not suffice, and
-// eight workers' 25.6M fp32 take 135 us instead of 117).
+// finite), or the products' warps do.  ONLY32: the same with nothing but fp32 to read (with the code for 16 bits beside it the
+// registers do not suffice, and eight workers' 25.6M fp32 take 135 us instead of 117).
 template <bool ADAM, bool ONLY32>
 __global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
 list_norm_kernel(const __grid_constant__ ListParams P)
@@ -573,28 +574,34 @@ list_norm_kernel(const __grid_constant__ ListParams P)
     double sum = sum_of_cta(s, red);
     if (threadIdx.x == 0) {
         __stcg(P.partial + (uint64_t)worker * gridDim.x + blockIdx.x, sum);
-        __threadfence();
-        last = atomicInc(P.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
+        last = blockIdx.x == 0 ? 1u : 0u;
+        if (P.partials == 0u) {
+            __threadfence();
+            last = atomicInc(P.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
+        }
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
     int64_t t = 0;
-    if (ADAM && (lane == 0u) && warp < 3u) {           // three threads of three warps at a time
+    if (ADAM && lane == 0u && warp < 3u) {             // three threads of three warps at a time
         t = (int64_t)load_base(reinterpret_cast<const uint64_t *>(P.adam.step)) + 1;
         if (warp == 1u) s_result.step_size = adam_step_size(P.adam, ld_global(P.adam.lr), t);
         if (warp == 2u) s_result.inv_sqrt_by2 = adam_inv_sqrt(P.adam, t);
     }
     sum = 0.0;
-    for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(P.partial + (uint64_t)worker * gridDim.x + i);
+    if (P.partials == 0u)
+        for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(P.partial + (uint64_t)worker * gridDim.x + i);
     sum = sum_of_cta(sum, red);                        // (with a barrier: the two sizes are there)
     if (threadIdx.x != 0) return;
-    const double norm = sqrt(sum);
-    P.norms[worker] = (float)norm;
-    s_result.c = factor_of(norm, P.max_norm);
-    s_result.stop = isfinite(norm) ? 0u : 1u;
-    if (!isfinite(norm)) atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
-    else if (ADAM) *P.adam.step = t;
+    if (P.partials == 0u) {
+        const double norm = sqrt(sum);
+        P.norms[worker] = (float)norm;
+        s_result.c = factor_of(norm, P.max_norm);
+        s_result.stop = isfinite(norm) ? 0u : 1u;
+        if (!isfinite(norm)) atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
+        else if (ADAM) *P.adam.step = t;
+    }
     if (P.result != nullptr) P.result[worker] = s_result;
 }
 
@@ -615,17 +622,31 @@ list_product_kernel(const __grid_constant__ ListParams P)
     float lr = 0.0f;
     uint4 q{};
     uint32_t stop = 0u;
+    double sum = 0.0;
     if (P.norms != nullptr) {
-        q = ld_global(reinterpret_cast<const uint4 *>(P.result + worker));
+        if (is_adam(K) || P.partials == 0u) q = ld_global(reinterpret_cast<const uint4 *>(P.result + worker));
         if (is_adam(K)) stop = ld_global(&P.result[worker].stop);
+        for (uint32_t i = lane; i < P.partials; i += 32u)
+            sum += __longlong_as_double((long long)load_base(reinterpret_cast<const uint64_t *>(P.partial + (uint64_t)worker * P.partials + i)));
     }
     if (is_adam(K)) lr = ld_global(P.adam.lr);
     const Early<K> early = load_early<K>(P, p, base, lane, kNotHeld);
     if (P.norms != nullptr) {
-        if (is_adam(K) && stop != 0u) return;          // the norm is not finite
         k.c = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
         k.step_size = __uint_as_float(q.z);
         k.inv_sqrt_by2 = __uint_as_float(q.w);
+        if (P.partials != 0u) {                        // the warp adds the worker's sums itself, all warps in the same order
+            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+            const double norm = sqrt(sum);
+            k.c = factor_of(norm, P.max_norm);
+            stop = isfinite(norm) ? 0u : 1u;
+            if (at % items == 0u && lane == 0u) {      // one warp per worker
+                P.norms[worker] = (float)norm;
+                if (stop != 0u) atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
+                else if (is_adam(K)) *P.adam.step = *P.adam.step + 1;
+            }
+        }
+        if (is_adam(K) && stop != 0u) return;          // the norm is not finite
     }
     if (is_adam(K)) adam_constants(P.adam, k);
     products<K>(P, p, base, early, worker, k, lr, lane, kNotHeld);
@@ -974,10 +995,12 @@ static void fill_params(ListParams &P, const thc_ctx *ctx, const thc_tensors *h,
     P.dev = view_of(ctx).dev;
 }
 
+static uint32_t split_of_norm(const thc_tensors *h) { return split_of(h, (uint64_t)h->sm_count * kListWarps / h->n); }
+
 template <bool ADAM>
 static int launch_norm(ListParams &P, const thc_tensors *h, cudaStream_t st)
 {
-    P.split_log2 = split_of(h, (uint64_t)h->sm_count * kListWarps / h->n);
+    P.split_log2 = split_of_norm(h);
     const dim3 grid(norm_ctas(h, P.split_log2), h->n);
     if (ADAM || P.src_flat != 0 || h->all_f32) THC_CUDA(launch_after(list_norm_kernel<ADAM, true>, grid, kListThreads, 0, st, P));
     else THC_CUDA(launch_after(list_norm_kernel<false, false>, grid, kListThreads, 0, st, P));
@@ -1002,6 +1025,8 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
 //   gather       4.3 / 6.9   4.5 / 7.0   5.2 / 7.0   5.2 / 6.9   8.2 / 6.9
 //   Adam step    6.2 / 8.7   7.9 / 8.6  10.2 / 8.5  10.4 / 8.4  17.9 / 8.3
 static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 32u : 64u; }
+
+constexpr uint32_t kOwnSumsMostPieces = 4096;
 
 template <ClipKind K>
 static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace, void *stream)
@@ -1031,6 +1056,8 @@ static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, 
         return THC_OK;
     }
     if (norms != nullptr) {
+        const uint32_t sums = norm_ctas(h, split_of_norm(h));
+        if ((uint64_t)h->pieces_n * h->n <= kOwnSumsMostPieces) P.partials = sums;
         const int rc = launch_norm<is_adam(K)>(P, h, st);
         if (rc != THC_OK) return rc;
     }
