@@ -273,9 +273,27 @@ static PyObject *b_prepare_noalloc(ARGS)
 }
 
 /* ---- lists of tensors.  What these calls take besides is as long as the list says; a torch tensor that is
- * shorter, of another type, not contiguous or elsewhere is refused here, as the library sees only its address. */
+ * shorter, of another type, not contiguous or elsewhere is refused here, as the library sees only its address.
+ *
+ * A call looks at up to nine tensors, five attributes each: asked for one by one through Python that takes 0.4 us a
+ * tensor, more than the launches of a small call.  torch describes a tensor in one C call through the exchange
+ * table of the DLPack standard (version 1.3: type and layout of the structures below are the standard's); where
+ * that is missing or does not want to, the attributes are asked for. */
+typedef struct { int32_t type, id; } dl_device;
+typedef struct { uint8_t code, bits; uint16_t lanes; } dl_type;
+typedef struct { void *data; dl_device device; int32_t ndim; dl_type dtype; int64_t *shape, *strides; uint64_t byte_offset; } dl_tensor;
+typedef struct {
+    uint32_t major, minor;
+    void *previous;
+    void *allocate, *managed_from_object, *managed_to_object;
+    int (*describe)(void *object, dl_tensor *out);
+    int (*current_stream)(int32_t device_type, int32_t device, void **out);
+} dl_exchange;
+enum { DL_CPU = 1, DL_CUDA = 2, DL_INT = 0, DL_FLOAT = 2, DL_BFLOAT = 4 };
+
 static PyObject *s_dtype, *s_is_contiguous, *s_get_device;
 static PyObject *tensor_type, *t_f32, *t_bf16, *t_i64;    /* of torch, looked up on first use */
+static const dl_exchange *exchange;                       /* null: attributes */
 
 static int torch_names(void)
 {
@@ -285,7 +303,14 @@ static int torch_names(void)
     if (tensor_type == NULL) tensor_type = PyObject_GetAttrString(m, "Tensor");
     if (t_f32 == NULL) t_f32 = PyObject_GetAttrString(m, "float32");
     if (t_bf16 == NULL) t_bf16 = PyObject_GetAttrString(m, "bfloat16");
-    if (tensor_type != NULL && t_f32 != NULL && t_bf16 != NULL) t_i64 = PyObject_GetAttrString(m, "int64");
+    if (tensor_type != NULL && t_f32 != NULL && t_bf16 != NULL) {
+        PyObject *c = PyObject_GetAttrString(tensor_type, "__dlpack_c_exchange_api__");
+        if (c != NULL) exchange = PyCapsule_GetPointer(c, "dlpack_exchange_api");
+        Py_XDECREF(c);                                    /* (the table is static) */
+        PyErr_Clear();
+        if (exchange != NULL && (exchange->major != 1 || exchange->describe == NULL)) exchange = NULL;
+        t_i64 = PyObject_GetAttrString(m, "int64");
+    }
     Py_DECREF(m);
     return t_i64 != NULL ? 0 : -1;
 }
@@ -300,32 +325,57 @@ static int list_of(PyObject *o, thc_tensors **list, thc_tensors_sizes_t *sz)
     return 0;
 }
 
+/* The stream of a call on a list: None is the current one of the list's device. */
+static int list_stream(PyObject *o, const thc_tensors_sizes_t *sz, void **st)
+{
+    if (o == Py_None && exchange != NULL && exchange->current_stream != NULL && sz->n != 0 && sz->device >= 0) {
+        if (exchange->current_stream(DL_CUDA, sz->device, st) == 0) return 0;
+        PyErr_Clear();
+    }
+    return stream_of(o, st);
+}
+
 enum { F32, BF16, I64 };
 static int vector(PyObject *o, void **p, int type, uint64_t elements, const thc_tensors_sizes_t *sz, const char *what)
 {
-    if (address(o, p) != 0) return -1;
-    if (o == Py_None || PyLong_Check(o) || sz->n == 0) return 0;
+    if (o == Py_None || PyLong_Check(o) || sz->n == 0) return address(o, p);
     const int is = PyObject_IsInstance(o, tensor_type);
-    if (is <= 0) return is;
-    PyObject *t = PyObject_GetAttr(o, s_dtype);
-    if (t == NULL) return -1;
-    const int same = t == (type == F32 ? t_f32 : type == BF16 ? t_bf16 : t_i64);
-    Py_DECREF(t);
-    PyObject *c = PyObject_CallMethodNoArgs(o, s_is_contiguous), *v = PyObject_GetAttr(o, s_nbytes),
-             *g = PyObject_CallMethodNoArgs(o, s_get_device);
-    uint64_t bytes = 0;
-    int ok = c != NULL && v != NULL && g != NULL && number(v, &bytes) == 0;
-    const long device = ok ? PyLong_AsLong(g) : 0;
-    if (PyErr_Occurred()) ok = 0;
-    if (ok && !(same && c == Py_True && bytes >= elements * (type == F32 ? 4u : type == BF16 ? 2u : 8u) && device == sz->device)) {
-        PyErr_Format(PyExc_ValueError, "%s: a contiguous %s tensor of at least %llu elements on the context's device is expected", what,
-                     type == F32 ? "float32" : type == BF16 ? "bfloat16" : "int64", (unsigned long long)elements);
-        ok = 0;
+    if (is < 0) return -1;
+    if (is == 0) return address(o, p);
+    int ok;
+    dl_tensor d;
+    memset(&d, 0, sizeof d);
+    if (exchange != NULL && exchange->describe(o, &d) == 0) {
+        uint64_t n = 1;
+        ok = 1;
+        for (int32_t i = d.ndim; i-- > 0;) {
+            if (d.strides != NULL && d.shape[i] > 1 && d.strides[i] != (int64_t)n) ok = 0;
+            n *= (uint64_t)d.shape[i];
+        }
+        const int cuda = d.device.type == DL_CUDA;
+        ok = ok && n >= elements && d.dtype.lanes == 1 && (cuda || d.device.type == DL_CPU) && (cuda ? d.device.id : -1) == sz->device &&
+             d.dtype.code == (type == F32 ? DL_FLOAT : type == BF16 ? DL_BFLOAT : DL_INT) && d.dtype.bits == (type == F32 ? 32 : type == BF16 ? 16 : 64);
+        *p = (char *)d.data + d.byte_offset;
+    } else {
+        PyErr_Clear();
+        if (address(o, p) != 0) return -1;
+        PyObject *t = PyObject_GetAttr(o, s_dtype), *c = PyObject_CallMethodNoArgs(o, s_is_contiguous), *v = PyObject_GetAttr(o, s_nbytes),
+                 *g = PyObject_CallMethodNoArgs(o, s_get_device);
+        uint64_t bytes = 0;
+        ok = t != NULL && c != NULL && v != NULL && g != NULL && number(v, &bytes) == 0;
+        const long device = ok ? PyLong_AsLong(g) : 0;
+        ok = ok && t == (type == F32 ? t_f32 : type == BF16 ? t_bf16 : t_i64) && c == Py_True && device == sz->device &&
+             bytes >= elements * (type == F32 ? 4u : type == BF16 ? 2u : 8u);
+        Py_XDECREF(t);
+        Py_XDECREF(c);
+        Py_XDECREF(v);
+        Py_XDECREF(g);
+        if (PyErr_Occurred()) return -1;
     }
-    Py_XDECREF(c);
-    Py_XDECREF(v);
-    Py_XDECREF(g);
-    return ok ? 0 : -1;
+    if (ok) return 0;
+    PyErr_Format(PyExc_ValueError, "%s: a contiguous %s tensor of at least %llu elements on the context's device is expected", what,
+                 type == F32 ? "float32" : type == BF16 ? "bfloat16" : "int64", (unsigned long long)elements);
+    return -1;
 }
 
 /* One vector per worker. */
@@ -355,26 +405,33 @@ static int real(PyObject *o, double *v)
     return *v == -1.0 && PyErr_Occurred() ? -1 : 0;
 }
 
-#define LIST_CALL thc_tensors *list; thc_tensors_sizes_t sz; uint64_t wb; void *ws
+/* `at`: the list's place among the arguments */
+#define LIST_CALL(count, at)                                                    \
+    void *ctx_p, *st, *ws;                                                      \
+    thc_tensors *list;                                                          \
+    thc_tensors_sizes_t sz;                                                     \
+    uint64_t wb;                                                                \
+    int rc;                                                                     \
+    (void)self;                                                                 \
+    if (want(na, count) || address(a[0], &ctx_p) || list_of(a[at], &list, &sz) || list_stream(a[na - 1], &sz, &st)) return NULL; \
+    thc_ctx *ctx = (thc_ctx *)ctx_p
 
 /* (handle, list, norms, workspace, stream) */
 static PyObject *b_grad_norm(ARGS)
 {
-    BEGIN(5);
-    LIST_CALL;
+    LIST_CALL(5, 1);
     void *norms;
-    if (list_of(a[1], &list, &sz) || vector(a[2], &norms, F32, sz.n, &sz, "norms") || workspace(a[3], &ws, &wb)) return NULL;
+    if (vector(a[2], &norms, F32, sz.n, &sz, "norms") || workspace(a[3], &ws, &wb)) return NULL;
     CALL(thc_grad_norm(ctx, list, norms, ws, wb, st));
 }
 
 /* (handle, list, max_norm, out, norms, workspace, stream) */
 static PyObject *b_clip_grads(ARGS)
 {
-    BEGIN(7);
-    LIST_CALL;
+    LIST_CALL(7, 1);
     double most;
     void *out, *norms;
-    if (list_of(a[1], &list, &sz) || real(a[2], &most) || address(a[3], &out) || vector(a[4], &norms, F32, sz.n, &sz, "norms") ||
+    if (real(a[2], &most) || address(a[3], &out) || vector(a[4], &norms, F32, sz.n, &sz, "norms") ||
         workspace(a[5], &ws, &wb)) return NULL;
     CALL(thc_clip_grads(ctx, list, most, out, norms, ws, wb, st));
 }
@@ -382,13 +439,12 @@ static PyObject *b_clip_grads(ARGS)
 /* (handle, list, max_norm, ef, flats, norms, workspace, bf16, stream) */
 static PyObject *b_gather_grads(ARGS)
 {
-    BEGIN(9);
-    LIST_CALL;
+    LIST_CALL(9, 1);
     double most;
     list_t e, f;
     void *norms;
     const int type = PyObject_IsTrue(a[7]) ? BF16 : F32;
-    if (list_of(a[1], &list, &sz) || real(a[2], &most) || vectors(a[3], &e, F32, &sz, "ef") || vectors(a[4], &f, type, &sz, "flats") ||
+    if (real(a[2], &most) || vectors(a[3], &e, F32, &sz, "ef") || vectors(a[4], &f, type, &sz, "flats") ||
         vector(a[5], &norms, F32, sz.n, &sz, "norms") || workspace(a[6], &ws, &wb)) return NULL;
     CALL(thc_gather_grads(ctx, list, most, (const float *const *)array_of(&e), array_of(&f), norms, ws, wb, st));
 }
@@ -396,11 +452,10 @@ static PyObject *b_gather_grads(ARGS)
 /* (handle, flat, max_norm, list, norms, workspace, stream) */
 static PyObject *b_scatter_grads(ARGS)
 {
-    BEGIN(7);
-    LIST_CALL;
+    LIST_CALL(7, 3);
     double most;
     void *flat, *norms;
-    if (list_of(a[3], &list, &sz) || vector(a[1], &flat, F32, sz.d, &sz, "flat") || real(a[2], &most) ||
+    if (vector(a[1], &flat, F32, sz.d, &sz, "flat") || real(a[2], &most) ||
         vector(a[4], &norms, F32, sz.n, &sz, "norms") || workspace(a[5], &ws, &wb)) return NULL;
     CALL(thc_scatter_grads(ctx, flat, most, list, norms, ws, wb, st));
 }
@@ -408,12 +463,11 @@ static PyObject *b_scatter_grads(ARGS)
 /* (handle, (beta1, beta2, eps, weight_decay, max_norm), grad, list, lr, step, master, m, v, decay, norms, workspace, stream) */
 static PyObject *b_adamw(ARGS)
 {
-    BEGIN(13);
-    LIST_CALL;
+    LIST_CALL(13, 3);
     thc_adamw_config cfg;
     void *grad, *lr, *step, *master, *m, *v, *decay, *norms;
     if (!PyArg_ParseTuple(a[1], "ddddd", &cfg.beta1, &cfg.beta2, &cfg.eps, &cfg.weight_decay, &cfg.max_norm)) return NULL;
-    if (list_of(a[3], &list, &sz) || vector(a[2], &grad, F32, sz.d, &sz, "grad") || vector(a[4], &lr, F32, 1, &sz, "lr") ||
+    if (vector(a[2], &grad, F32, sz.d, &sz, "grad") || vector(a[4], &lr, F32, 1, &sz, "lr") ||
         vector(a[5], &step, I64, 1, &sz, "step") || vector(a[6], &master, F32, sz.d, &sz, "master") ||
         vector(a[7], &m, F32, sz.d, &sz, "m") || vector(a[8], &v, F32, sz.d, &sz, "v") ||
         vector(a[9], &decay, F32, sz.count, &sz, "decay") || vector(a[10], &norms, F32, 1, &sz, "norms") || workspace(a[11], &ws, &wb)) return NULL;

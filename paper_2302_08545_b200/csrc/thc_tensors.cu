@@ -444,8 +444,10 @@ struct ListParams {
     NormResult *result;          // workspace: one per worker
     DeviceBlock *dev;
     AdamParams adam;
-    uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS];   // kGather*
 };
+struct GatherParams : ListParams { uint64_t dst_flat[THC_MAX_WORKERS], ef[THC_MAX_WORKERS]; };
+// (1 KB less to hand over where it is not needed)
+template <ClipKind K> using ParamsOf = std::conditional_t<K == kGatherF32 || K == kGatherBf16 || K == kGatherResidual, GatherParams, ListParams>;
 
 // Part `item` of all parts of the pieces; length 0 where a piece is too short to have it.
 __device__ __forceinline__ Piece load_item(const ListTable &L, uint32_t item, uint32_t split_log2)
@@ -467,14 +469,14 @@ __device__ __forceinline__ ItemBase load_item_base(const ListParams &P, const Pi
 }
 
 template <ClipKind K, uint32_t T>
-__device__ __forceinline__ void move_typed(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t worker, const Factor &c, uint32_t lane,
+__device__ __forceinline__ void move_typed(const ParamsOf<K> &P, const Piece &p, const ItemBase &base, uint32_t worker, const Factor &c, uint32_t lane,
                                            uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu;
     const uint64_t at = p.flat * size_of<T>(), tensor = base.tensor + at;
-    if (K == kClip) {
+    if constexpr (K == kClip) {
         move_piece<T, T, false>(tensor, base.dst + at, 0, len, len, c, lane, held);
-    } else if (K == kScatter) {
+    } else if constexpr (K == kScatter) {
         move_piece<THC_F32, T, false>(P.src_flat + p.flat * 4u, tensor, 0, len, len, c, lane, held);
     } else {
         constexpr uint32_t D = K == kGatherBf16 ? THC_BF16 : THC_F32;
@@ -505,7 +507,7 @@ __device__ __forceinline__ Early<K> load_early(const ListParams &P, const Piece 
 }
 
 template <ClipKind K>
-__device__ __forceinline__ void products(const ListParams &P, const Piece &p, const ItemBase &base, const Early<K> &early, uint32_t worker, AdamStep &k,
+__device__ __forceinline__ void products(const ParamsOf<K> &P, const Piece &p, const ItemBase &base, const Early<K> &early, uint32_t worker, AdamStep &k,
                                          float lr, uint32_t lane, uint32_t held)
 {
     const uint32_t type = p.len_type >> 16;
@@ -608,7 +610,7 @@ list_norm_kernel(const __grid_constant__ ListParams P)
 // Products of eight items to a CTA, over all workers; the last ones first.
 template <ClipKind K>
 __global__ void __launch_bounds__(kListThreads, product_ctas_per_sm(K))
-list_product_kernel(const __grid_constant__ ListParams P)
+list_product_kernel(const __grid_constant__ ParamsOf<K> P)
 {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint32_t items = P.L.pieces_n << P.split_log2, all = items * P.n, j = blockIdx.x * kListWarps + warp;
@@ -656,7 +658,7 @@ list_product_kernel(const __grid_constant__ ListParams P)
 // each adds them in the same order and forms norm and factor itself.  A warp's last item is still in its shared memory.
 template <ClipKind K>
 __global__ void __launch_bounds__(kClusterThreads, 1)
-list_cluster_kernel(const __grid_constant__ ListParams P)
+list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
 {
     extern __shared__ __align__(16) unsigned char held_bytes[];
     __shared__ double red[kClusterWarps], sums[kClusterCtas];
@@ -1002,7 +1004,7 @@ static int launch_norm(ListParams &P, const thc_tensors *h, cudaStream_t st)
 {
     P.split_log2 = split_of_norm(h);
     const dim3 grid(norm_ctas(h, P.split_log2), h->n);
-    if (ADAM || P.src_flat != 0 || h->all_f32) THC_CUDA(launch_after(list_norm_kernel<ADAM, true>, grid, kListThreads, 0, st, P));
+    if (ADAM || P.src_flat != 0 || h->all_f32) THC_CUDA(launch_after(list_norm_kernel<ADAM, true>, grid, kListThreads, 0, st, static_cast<const ListParams &>(P)));
     else THC_CUDA(launch_after(list_norm_kernel<false, false>, grid, kListThreads, 0, st, P));
     return THC_OK;
 }
@@ -1029,7 +1031,7 @@ static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 
 constexpr uint32_t kOwnSumsMostPieces = 4096;
 
 template <ClipKind K>
-static int launch_call(ListParams &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace, void *stream)
+static int launch_call(ParamsOf<K> &P, const thc_ctx *ctx, const thc_tensors *h, double max_norm, float *norms, void *workspace, void *stream)
 {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     fill_params(P, ctx, h, max_norm, norms, workspace);
@@ -1109,7 +1111,7 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
     if (bf16 && ef_or_null != nullptr) return THC_EUNSUPPORTED;
     if (flats == nullptr) return THC_EINVAL;
     const uint64_t bytes = list->d * (bf16 ? 2u : 4u);
-    ListParams P;
+    GatherParams P;
     memset(&P, 0, sizeof P);
     for (uint32_t i = 0; i < list->n; ++i) {
         if (flats[i] == nullptr || !aligned16(flats[i])) return THC_EINVAL;
