@@ -28,7 +28,7 @@ namespace thc {
 constexpr uint32_t kPiece = 2048;              // elements of a piece: eight units of eight per lane
 constexpr uint32_t kUnit = 8;                  // consecutive elements of a lane: 16 bytes of a 16-bit type, 32 of fp32
 constexpr int kListThreads = 256, kListWarps = kListThreads / 32;
-constexpr uint32_t kNormCtasPerSm = 4;
+constexpr uint32_t kNormCtasPerSm = 4, kNormMostRows = 8, kNormLeastRounds = 6;
 constexpr int kClusterThreads = 512, kClusterWarps = kClusterThreads / 32;
 constexpr uint32_t kClusterCtas = 8;
 constexpr uint32_t kHeldBytes = 4096;          // per warp: half a piece of fp32, which is the most that a warp of the cluster takes at a time
@@ -440,6 +440,7 @@ struct ListParams {
     double max_norm;
     float *norms;                // or null: no norm, factor 1
     double *partial;             // workspace: a sum per CTA
+    uint32_t row, rounds;        // list_norm_kernel: see there
     uint32_t partials;           // sums per worker that list_product_kernel adds itself, or 0: it finds the result
     NormResult *result;          // workspace: one per worker
     DeviceBlock *dev;
@@ -547,8 +548,10 @@ __device__ __forceinline__ double power(double beta, uint64_t t)
 __device__ __forceinline__ float adam_step_size(const AdamParams &a, float lr, int64_t t) { return (float)((double)lr / (1.0 - power(a.beta1, (uint64_t)t))); }
 __device__ __forceinline__ float adam_inv_sqrt(const AdamParams &a, int64_t t) { return (float)(1.0 / sqrt(1.0 - power(a.beta2, (uint64_t)t))); }
 
-// Sums of squares, grid (CTAs of a worker, workers).  A warp's pieces are fixed by the grid and the sums are added in a fixed
-// order; a worker's last CTA does that and forms what the products need (ADAM: also the step count, unless the norm is not
+// Sums of squares, grid (CTAs of a worker, workers).  A warp's pieces are fixed by the grid: `row` CTAs, as many as run at a
+// time, go side by side through `rounds` rounds of pieces, the next row of CTAs through the next rounds.  (One row for all of
+// it drifts apart, which DRAM minds while the last launch's writes still leave L2: 355M scattered 526 us, in eight rows 507;
+// eight workers gathered 380, 366.)  The sums are added in a fixed order; a worker's last CTA does that and forms what the products need (ADAM: also the step count, unless the norm is not
 // finite), or the products' warps do.  ONLY32: the same with nothing but fp32 to read (with the code for 16 bits beside it the
 // registers do not suffice, and eight workers' 25.6M fp32 take 135 us instead of 117).
 template <bool ADAM, bool ONLY32>
@@ -556,18 +559,19 @@ __global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
 list_norm_kernel(const __grid_constant__ ListParams P)
 {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
-    const uint32_t stride = gridDim.x * kListWarps, items = P.L.pieces_n << P.split_log2;
-    uint32_t c = blockIdx.x * kListWarps + warp;
+    const uint32_t stride = P.row * kListWarps, from = blockIdx.x / P.row * P.rounds * stride;
+    const uint32_t end = min(P.L.pieces_n << P.split_log2, from + P.rounds * stride);
+    uint32_t c = from + blockIdx.x % P.row * kListWarps + warp;
     Piece p{};
-    if (c < items) p = load_item(P.L, c, P.split_log2);     // written before any launch
+    if (c < end) p = load_item(P.L, c, P.split_log2);       // written before any launch
     depend_on_previous();
     const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
     double s = 0.0;
 #pragma unroll 1
-    while (c < items) {
+    while (c < end) {
         const Piece now = p;
         c += stride;
-        if (c < items) p = load_item(P.L, c, P.split_log2);
+        if (c < end) p = load_item(P.L, c, P.split_log2);
         s += squares<false, ONLY32>(now, base, P.src_flat, lane, kNotHeld);
     }
     __shared__ double red[kListWarps];
@@ -593,6 +597,7 @@ list_norm_kernel(const __grid_constant__ ListParams P)
     }
     sum = 0.0;
     if (P.partials == 0u)
+#pragma unroll 4
         for (uint32_t i = threadIdx.x; i < gridDim.x; i += kListThreads) sum += __ldcg(P.partial + (uint64_t)worker * gridDim.x + i);
     sum = sum_of_cta(sum, red);                        // (with a barrier: the two sizes are there)
     if (threadIdx.x != 0) return;
@@ -883,11 +888,19 @@ int thc_tensors_destroy(thc_tensors *h)
     return THC_OK;
 }
 
-// CTAs per worker of the sums.
-static uint32_t norm_ctas(const thc_tensors *h, uint32_t split_log2)
+// CTAs per worker of the sums: rows of as many as run at a time (see list_norm_kernel), each of them at least six rounds long; one
+// row where nothing is written after them (355M bf16, us: 112, in six rows 117; fp32 of the same bytes 103, 105).
+struct NormShape { uint32_t row, rounds, ctas; };
+static NormShape norm_shape(const thc_tensors *h, uint32_t split_log2, bool alone)
 {
     const uint32_t most = std::max(1u, h->sm_count * kNormCtasPerSm / h->n);
-    return (uint32_t)std::min<uint64_t>(most, (((uint64_t)h->pieces_n << split_log2) + kListWarps - 1) / kListWarps);
+    const uint64_t groups = (((uint64_t)h->pieces_n << split_log2) + kListWarps - 1) / kListWarps;
+    NormShape s;
+    s.row = (uint32_t)std::min<uint64_t>(most, groups);
+    const uint32_t rounds = (uint32_t)((groups + s.row - 1) / s.row), rows = alone ? 1u : std::min(std::max(rounds / kNormLeastRounds, 1u), kNormMostRows);
+    s.rounds = (rounds + rows - 1) / rows;
+    s.ctas = (rounds + s.rounds - 1) / s.rounds * s.row;
+    return s;
 }
 
 static uint64_t round_up256(uint64_t v) { return (v + 255) / 256 * 256; }
@@ -895,7 +908,7 @@ static uint64_t round_up256(uint64_t v) { return (v + 255) / 256 * 256; }
 // Workspace: results of the workers, then the sums' partial results.
 static uint64_t workspace_need(const thc_tensors *h)
 {
-    return round_up256(h->n * sizeof(NormResult)) + round_up256((uint64_t)h->n * norm_ctas(h, 3) * sizeof(double));
+    return round_up256(h->n * sizeof(NormResult)) + round_up256((uint64_t)h->n * std::max(norm_shape(h, 0, false).ctas, norm_shape(h, 3, false).ctas) * sizeof(double));
 }
 
 int thc_tensors_sizes(const thc_tensors *h, thc_tensors_sizes_t *s)
@@ -1000,10 +1013,13 @@ static void fill_params(ListParams &P, const thc_ctx *ctx, const thc_tensors *h,
 static uint32_t split_of_norm(const thc_tensors *h) { return split_of(h, (uint64_t)h->sm_count * kListWarps / h->n); }
 
 template <bool ADAM>
-static int launch_norm(ListParams &P, const thc_tensors *h, cudaStream_t st)
+static int launch_norm(ListParams &P, const thc_tensors *h, bool alone, cudaStream_t st)
 {
     P.split_log2 = split_of_norm(h);
-    const dim3 grid(norm_ctas(h, P.split_log2), h->n);
+    const NormShape shape = norm_shape(h, P.split_log2, alone);
+    P.row = shape.row;
+    P.rounds = shape.rounds;
+    const dim3 grid(shape.ctas, h->n);
     if (ADAM || P.src_flat != 0 || h->all_f32) THC_CUDA(launch_after(list_norm_kernel<ADAM, true>, grid, kListThreads, 0, st, static_cast<const ListParams &>(P)));
     else THC_CUDA(launch_after(list_norm_kernel<false, false>, grid, kListThreads, 0, st, P));
     return THC_OK;
@@ -1019,7 +1035,7 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
     memset(&P, 0, sizeof P);
     fill_params(P, ctx, list, INFINITY, norms, workspace);
     P.result = nullptr;
-    return launch_norm<false>(P, list, static_cast<cudaStream_t>(stream));
+    return launch_norm<false>(P, list, true, static_cast<cudaStream_t>(stream));
 }
 
 // Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
@@ -1058,9 +1074,8 @@ static int launch_call(ParamsOf<K> &P, const thc_ctx *ctx, const thc_tensors *h,
         return THC_OK;
     }
     if (norms != nullptr) {
-        const uint32_t sums = norm_ctas(h, split_of_norm(h));
-        if ((uint64_t)h->pieces_n * h->n <= kOwnSumsMostPieces) P.partials = sums;
-        const int rc = launch_norm<is_adam(K)>(P, h, st);
+        if ((uint64_t)h->pieces_n * h->n <= kOwnSumsMostPieces) P.partials = norm_shape(h, split_of_norm(h), false).ctas;
+        const int rc = launch_norm<is_adam(K)>(P, h, false, st);
         if (rc != THC_OK) return rc;
     }
     P.split_log2 = split_of(h, (uint64_t)h->sm_count * product_ctas_per_sm(K) * kListWarps / h->n);

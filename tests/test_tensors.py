@@ -135,9 +135,9 @@ for n in (1, 4):
 h = lst([300_000_001], [1])
 assert call("thc_clip_grads", h, 1.0, None, N) == 0
 got = rows()
-assert got[0][1][:2] == [592, 256] and got[1][1][:2] == [-(-(-(-300_000_001 // 2048)) // 8), 256], got
+assert got[0][1][:2] == [5 * 592, 256] and got[1][1][:2] == [-(-(-(-300_000_001 // 2048)) // 8), 256], got
 assert call("thc_grad_norm", h, N) == 0
-assert [g[0] for g in rows()] == ["norm_"]
+assert [(g[0], g[1][0]) for g in rows()] == [("norm_", 592)]
 # addresses anew: 448 to a launch
 h = lst([5] * 1000, [0] * 1000)
 assert L.thc_tensors_assign(c._h, h, p(*[(1 << 40) + 64 * i for i in range(1000)]), None) == 0
