@@ -1,6 +1,7 @@
 """A round between a program's tensors on the GPU, used as a training step would: gradients of many tensors of mixed types,
 clipped and gathered, through the round (against the same round on vectors made with torch), the residual of error feedback over
 rounds, and the average into weights by an Adam step or into tensors; on one GPU and through the data-parallel path."""
+import gc
 import math
 import os
 import socket
@@ -12,6 +13,14 @@ import tensor_lists as T
 from tensor_lists import U
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def nothing_left_behind():
+    """What a caught exception's frames hold (tensors) goes with the test, not in the middle of a later one."""
+    yield
+    gc.collect()
+
 
 SIZES = [40_000, 1, 333, 64, 7_001, 20_000, 5]
 

@@ -6,6 +6,7 @@ levels, each of which is off by at most u of a sum of positive terms, 3 u in all
 off by half of that, before(list) = 1.5 u, or 0 without 16-bit tensors.  It is rounded to fp32 (u).  The factor is formed in fp64
 from the norm before that rounding, so it is off by before(list), and rounded (u); the product is rounded (u), then once more to
 the tensor's type.  The Adam step's bounds are beside its test."""
+import gc
 import math
 
 import pytest
@@ -15,6 +16,14 @@ import tensor_lists as T
 from tensor_lists import TYPES, U
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def nothing_left_behind():
+    """What a caught exception's frames hold (tensors) goes with the test, not in the middle of a later one."""
+    yield
+    gc.collect()
+
 
 EDGES = [1, 7, 0, 8, 9, 63, 64, 65, 255, 1000, 2047, 2048, 2049, 4096 + 17, 100_003]
 SMALL = 1.0 + 2.0 ** -16               # second-order terms of the bounds
