@@ -69,6 +69,7 @@ extern "C" {
 
 /* thc_status() bits */
 #define THC_STATUS_NONFINITE     1u  /* a block's norm was NaN/Inf: its scale was set to 0        */
+                                     /* (lists of tensors: a worker's norm was)                    */
 #define THC_STATUS_ZERO_BLOCK    2u  /* a block had scale 0 (all-zero input): indices 0, output 0 */
                                      /* (exact range: a block whose range is [0, 0])              */
 #define THC_STATUS_WAIT_TIMEOUT  4u  /* an on-device wait gave up; the call's output is invalid   */
@@ -279,7 +280,8 @@ int thc_accumulate_error(thc_ctx *ctx, float *const *grads, const float *const *
  * of a list starts at offsets[t], a multiple of THC_TENSOR_ALIGN elements; the up to THC_TENSOR_ALIGN - 1
  * elements between one tensor's end and the next one's start belong to no tensor.  The calls below
  * take tensors at any address that suits their type.  A list is a plan that a program keeps: it holds
- * addresses, not the tensors, which stay the caller's. */
+ * addresses, not the tensors, which stay the caller's.  Calls on it are served on the device it was made for, by any
+ * context of that device; their workspace (sizes.workspace_bytes) is scratch from the call's start to its end. */
 #define THC_TENSOR_ALIGN 64u
 
 typedef struct thc_tensors thc_tensors;   /* opaque */
@@ -354,14 +356,14 @@ int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const th
  * rate and step count are read on the device, so that a captured step can be replayed.
  *   grad    device, sizes.d fp32, read
  *   list    n = 1: the model's weights, written
- *   lr      device, one fp32;   step  device, one int64 (steps done so far), t is written back
+ *   lr      device, one fp32;   step  device, one int64 (steps done so far, >= 0), t is written back
  *   master  device, sizes.d fp32: w, from which the tensors are rounded; NULL: the tensors are w
  *           themselves and all of them fp32 (THC_EINVAL otherwise)
  *   m, v    device, sizes.d fp32 each
  *   decay_or_null  device, `count` fp32: wd of each tensor (NULL: cfg.weight_decay for all)
  *   norms   device, one fp32, written
- * Nothing that is written may overlap anything else (THC_EINVAL); between the tensors master, m and v are
- * neither read nor written. */
+ * master, m, v, grad and the tensors must not overlap each other (THC_EINVAL); between the tensors master, m and v
+ * are neither read nor written.  With eps = 0 an element whose gradients have all been 0 divides 0 by 0. */
 typedef struct thc_adamw_config {
     double beta1, beta2;       /* 0 <= beta < 1                             */
     double eps;                /* >= 0                                      */

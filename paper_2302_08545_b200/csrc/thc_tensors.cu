@@ -551,9 +551,10 @@ __device__ __forceinline__ float adam_inv_sqrt(const AdamParams &a, int64_t t) {
 // Sums of squares, grid (CTAs of a worker, workers).  A warp's pieces are fixed by the grid: `row` CTAs, as many as run at a
 // time, go side by side through `rounds` rounds of pieces, the next row of CTAs through the next rounds.  (One row for all of
 // it drifts apart, which DRAM minds while the last launch's writes still leave L2: 355M scattered 526 us, in eight rows 507;
-// eight workers gathered 380, 366.)  The sums are added in a fixed order; a worker's last CTA does that and forms what the products need (ADAM: also the step count, unless the norm is not
-// finite), or the products' warps do.  ONLY32: the same with nothing but fp32 to read (with the code for 16 bits beside it the
-// registers do not suffice, and eight workers' 25.6M fp32 take 135 us instead of 117).
+// eight workers gathered 380, 366.)  The sums are added in a fixed order; a worker's last CTA does that and forms what the products
+// need (ADAM: also the step count, unless the norm is not finite), or the products' warps do.  ONLY32: the same with nothing but
+// fp32 to read (with the code for 16 bits beside it the registers do not suffice, and eight workers' 25.6M fp32 take 135 us
+// instead of 117).
 template <bool ADAM, bool ONLY32>
 __global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
 list_norm_kernel(const __grid_constant__ ListParams P)
@@ -580,7 +581,7 @@ list_norm_kernel(const __grid_constant__ ListParams P)
     double sum = sum_of_cta(s, red);
     if (threadIdx.x == 0) {
         __stcg(P.partial + (uint64_t)worker * gridDim.x + blockIdx.x, sum);
-        last = blockIdx.x == 0 ? 1u : 0u;
+        last = ADAM && blockIdx.x == 0 ? 1u : 0u;      // (for the two sizes)
         if (P.partials == 0u) {
             __threadfence();
             last = atomicInc(P.dev->norm_counters + worker, gridDim.x - 1u) == gridDim.x - 1u;
@@ -674,6 +675,7 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
     uint32_t c = first;
     Piece last{}, p{};
     ItemBase last_base{};
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this CTA runs: the others may write to it
     if (c < items) p = load_item(P.L, c, P.split_log2);     // written before any launch
     depend_on_previous();
     const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
@@ -699,12 +701,15 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
     Early<K> early{};
     if (first < items) early = load_early<K>(P, last, last_base, lane, held);
     const double sum = sum_of_cta(s, red);
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");             // all CTAs run
     if (threadIdx.x == 0) {
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x]);
 #pragma unroll
         for (uint32_t r = 0; r < kClusterCtas; ++r)
             asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f64 [a], %2;\n\t}" :: "r"(to), "r"(r), "d"(sum) : "memory");
     }
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x == 0) {

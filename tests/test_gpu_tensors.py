@@ -58,7 +58,8 @@ LISTS = [
     ([1], ["f32"], 1, 0), ([1], ["f16"], 3, 1), ([5], ["bf16"], 1, 3), (EDGES, ["f32"], 1, 0), (EDGES, ["bf16"], 2, 0),
     (EDGES, ["f16"], 1, 0), (EDGES, ["f32", "bf16", "f16", "bf16"], 3, 0), (EDGES, ["f32"], 2, 1), (EDGES, ["bf16"], 1, 4),
     (EDGES, ["f16"], 2, 2), (EDGES, ["f16", "f32"], 1, 5), ([300_001, 2_000_003], ["f32"], 5, 0), ([7_000_003], ["bf16"], 1, 0),
-    ([17] * 400, ["f32", "bf16"], 2, 0), ([4096] * 64, ["bf16"], 64, 0),
+    ([17] * 400, ["f32", "bf16"], 2, 0), ([4096] * 64, ["bf16"], 64, 0), ([2000, 100, 7], ["f32", "f16"], 64, 0), ([131_072], ["f32"], 1, 0),
+    ([131_073], ["f32"], 1, 0), ([1025] * 64, ["bf16"], 3, 0), ([8_388_608], ["bf16"], 1, 0), ([8_388_609], ["f32"], 1, 0), ([20_000_001, 9], ["f16"], 1, 0),
 ]
 
 
@@ -468,3 +469,85 @@ def test_refused_arguments():
         ctx.clip_grads(one, 1.0, norms, ws, out=half)
     assert code(lambda: ctx.grad_norm(half, norms, ws)) == EINVAL
     torch.cuda.synchronize()
+
+
+def test_positions_past_32_bits():
+    """More than 2^31 elements of 16 bits and 2^33 bytes of fp32 before the last tensors."""
+    big = 2 ** 31 + 2049
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    x = torch.empty(big, dtype=torch.bfloat16, device="cuda")
+    for part in x.split(1 << 28):
+        part.normal_()
+    workers = [[x, torch.randn(1000, device="cuda"), torch.randn(77, device="cuda").half()]]
+    ctx, lst, norms, ws = setup(workers)
+    flat = torch.full((lst.d,), 9.0, device="cuda")
+    ctx.gather_grads(lst, 1000.0, [flat], norms, ws)
+    square = sum(float((p.double() ** 2).sum()) for t in workers[0] for p in t.split(1 << 26))
+    norm = math.sqrt(square)
+    assert abs(float(norms) - norm) <= norm * 2.6 * U
+    c = T.factor(norm, 1000.0)
+    for t, v in zip(workers[0], lst.views(flat)):
+        for a, b in zip(t.split(1 << 28), v.split(1 << 28)):
+            exact = a.double() * c
+            T.within(b, exact, exact.abs() * 4.6 * U + 2.0 ** -149)
+    assert not bool(flat[big: lst.offsets[1]].any())
+    back = [[torch.zeros_like(x), torch.zeros(1000, device="cuda"), torch.zeros(77, device="cuda").half()]]
+    from paper_2302_08545_b200 import thc
+    ctx.scatter_grads(flat, math.inf, thc.Tensors(ctx, back), None, None)
+    for t, v in zip(back[0], lst.views(flat)):
+        for a, b in zip(t.split(1 << 28), v.split(1 << 28)):
+            assert torch.equal(a, b.to(a.dtype))
+
+
+def test_values_past_the_end_of_16_bits():
+    """fp32 values that fp16 and bf16 do not hold become infinite, as a rounding to nearest says."""
+    from paper_2302_08545_b200 import thc
+    workers = [[torch.zeros(100, device="cuda").half(), torch.zeros(100, device="cuda").bfloat16(), torch.zeros(100, device="cuda")]]
+    ctx, lst, norms, ws = setup(workers)
+    flat = torch.zeros(lst.d, device="cuda")
+    for v in lst.views(flat):
+        v[:4] = torch.tensor([65519.0, 65520.0, -7e4, 3.4e38], device="cuda")
+    ctx.scatter_grads(flat, math.inf, lst, norms, ws)
+    for x, v in zip(workers[0], lst.views(flat)):
+        assert torch.equal(x, v.to(x.dtype))
+    assert ctx.status() == 0
+
+
+@pytest.mark.parametrize("steps", [0, 1, 1000, 10 ** 6, 2 ** 40])
+@pytest.mark.parametrize("size", [100, 300_000])
+def test_adamw_after_many_steps(steps, size):
+    """1 - beta^t after few and very many steps."""
+    workers = T.make([size], ["f32"], 1, seed=7)
+    ctx, lst, norms, ws = setup(workers)
+    grad, m, v = (torch.rand(lst.d, device="cuda") + 0.5 for _ in range(3))
+    w0, m0, v0 = workers[0][0].double(), lst.views(m)[0].double(), lst.views(v)[0].double()
+    lr, step = torch.full((1,), 1e-2, device="cuda"), torch.full((1,), steps, dtype=torch.int64, device="cuda")
+    ctx.adamw(grad, lst, lr, step, m, v, norms, ws, betas=(0.9, 0.999), eps=1e-8, max_norm=math.inf)
+    assert int(step) == steps + 1
+    m2, v2, w2, dm, dv, dw = adam_exact(lst.views(grad)[0].double(), m0, v0, w0, 1.0, steps + 1, float(lr), 0.0, 0.9, 0.999, 1e-8)
+    T.within(lst.views(m)[0], m2, dm)
+    T.within(lst.views(v)[0], v2, dv)
+    T.within(workers[0][0], w2, dw)
+
+
+def test_many_calls_in_a_row_of_every_length():
+    """Clusters, sums that the products add themselves and sums that the last CTA adds, one after the other on one context, with
+    nothing between: every call's norm is its own."""
+    from paper_2302_08545_b200 import thc
+    ctx = context()
+    cases = []
+    for i, size in enumerate([100, 5_000_000, 70_000, 9_000_001, 131_073, 3]):
+        workers = T.make([size, 65], ["f32", "bf16"], 1 + i % 3, seed=i)
+        lst = thc.Tensors(ctx, workers)
+        cases.append((workers, lst, [torch.empty(lst.d, device="cuda") for _ in workers]))
+    ws = torch.empty(max(c[1].workspace_bytes for c in cases), dtype=torch.uint8, device="cuda")
+    norms = torch.zeros(40, len(cases), 3, device="cuda")
+    for r in range(40):
+        for i, (workers, lst, flats) in enumerate(cases):
+            ctx.gather_grads(lst, 1.0, flats, norms[r, i, : lst.n], ws)
+    for i, (workers, lst, flats) in enumerate(cases):
+        ref = torch.tensor([T.norm(w) for w in workers], dtype=torch.float64)
+        T.within(norms[0, i, : lst.n].cpu(), ref, ref * 2.6 * U)
+        assert bool((norms[:, i] == norms[0, i]).all())
+    assert ctx.status() == 0
