@@ -1045,9 +1045,9 @@ int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *wor
 
 // Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
 //   pieces          16          32          48          64          96
-//   gather       4.3 / 6.9   4.5 / 7.0   5.2 / 7.0   5.2 / 6.9   8.2 / 6.9
-//   Adam step    6.2 / 8.7   7.9 / 8.6  10.2 / 8.5  10.4 / 8.4  17.9 / 8.3
-static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 32u : 64u; }
+//   gather       4.3 / 6.0   4.6 / 5.6   5.2 / 5.6   5.3 / 5.7   8.3 / 5.8
+//   Adam step    6.2 / 6.7   7.8 / 6.7  10.1 / 7.2  10.3 / 7.3  17.0 / 7.8
+static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 16u : 64u; }
 
 constexpr uint32_t kOwnSumsMostPieces = 4096;
 

@@ -19,6 +19,9 @@ buffer), warms the calls up, times them with CUDA events and prints one JSON lin
   fused             thc_prepare_compress, n = 8 (thc_pipeline_kernel<fused scales + compress>)
   scan              compress, decompress and error feedback of 4 x 2^26 fp32 coordinates for B = 2^8 .. 2^22 (a
                     line each; blocks held in shared memory up to 2^15, the two-pass pipeline above)
+  tensors           lists of 40 tensors, 2^26 elements: norm of fp32 and bf16, clip of bf16, gather of fp32, scatter to bf16
+                    and the Adam step with bf16 weights (list_norm_kernel, list_product_kernel; a line each), and the
+                    same calls on 2^16 elements (list_cluster_kernel; the Adam step's two kernels)
   cfg1 .. cfg4, cfg3b2   the benchmark configurations at full size, inputs generated on the device
                     (per-call times of the round, error feedback and the one-call tail included)
 """
@@ -72,11 +75,43 @@ def scan(iters: int):
         torch.cuda.empty_cache()
 
 
+def tensors(iters: int):
+    """The calls on lists of tensors, long and short ones."""
+    import numpy as np
+    import torch
+    from . import runner, thc
+    stream = torch.cuda.current_stream()
+    w = W.Workload("profile_tensors", n=1, d=1 << 16, log2_block=12, bits=4, granularity=30, table=W.TABLES[(4, 30)], data_seed=9)
+    ctx = runner.context_for(w)
+    for d in (1 << 26, 1 << 16):
+        share = np.random.default_rng(9).lognormal(0.0, 1.5, 40)
+        sizes = np.maximum(1, (share / share.sum() * d).astype(np.int64)).tolist()
+        make = lambda dtype: [torch.randn(s, device="cuda").to(dtype) for s in sizes]
+        f32, bf16 = thc.Tensors(ctx, [make(torch.float32)]), thc.Tensors(ctx, [make(torch.bfloat16)])
+        out = thc.Tensors(ctx, [make(torch.bfloat16)])
+        flat, m, v, master = (torch.rand(f32.d, device="cuda") for _ in range(4))
+        norms, lr = torch.zeros(1, device="cuda"), torch.full((1,), 1e-3, device="cuda")
+        step = torch.zeros(1, dtype=torch.int64, device="cuda")
+        ws = torch.empty(f32.workspace_bytes, dtype=torch.uint8, device="cuda")
+        n = f32.elements
+        for name, nbytes, call in (("grad_norm f32", 4 * n, lambda: ctx.grad_norm(f32, norms, ws)),
+                                   ("grad_norm bf16", 2 * n, lambda: ctx.grad_norm(bf16, norms, ws)),
+                                   ("clip_grads bf16", 4 * n, lambda: ctx.clip_grads(bf16, 1.0, norms, ws, out=out)),
+                                   ("gather_grads f32", 8 * n, lambda: ctx.gather_grads(f32, 1.0, [flat], norms, ws)),
+                                   ("scatter_grads bf16", 6 * n, lambda: ctx.scatter_grads(flat, 1.0, out, norms, ws)),
+                                   ("adamw bf16", 30 * n, lambda: ctx.adamw(flat, out, lr, step, m, v, norms, ws, master=master, max_norm=1.0))):
+            ms = _time(call, iters, torch, stream)
+            print(json.dumps({"case": "tensors", "call": name, "elements": n, "ms": round(ms, 4), "algorithmic_gbs": round(nbytes / ms / 1e6, 1),
+                              "status_flags": ctx.status()}), flush=True)
+
+
 def run(case: str, iters: int):
     import torch
     from . import runner
     if case == "scan":
         return scan(iters)
+    if case == "tensors":
+        return tensors(iters)
     stream = torch.cuda.current_stream()
     T = W.TABLES[(4, 30)]
     mk = lambda **kw: W.Workload(f"profile_{case}", table=kw.pop("table", T), bits=kw.pop("bits", 4),
@@ -136,7 +171,7 @@ def run(case: str, iters: int):
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["tile14", "quantize", "bf16k22", "n16", "b2", "ef", "minmax", "aggdec", "fused", "scan",
+    ap.add_argument("case", choices=["tile14", "quantize", "bf16k22", "n16", "b2", "ef", "minmax", "aggdec", "fused", "scan", "tensors",
                                      "cfg1", "cfg2", "cfg3", "cfg3b2", "cfg4"])
     ap.add_argument("--iters", type=int, default=5)
     a = ap.parse_args()
