@@ -295,8 +295,8 @@ typedef struct thc_tensors_sizes_t {
     int32_t device;            /* the context's, -1 without one                                */
 } thc_tensors_sizes_t;
 
-/* Make a list.  With a device, allocates device memory for its tables (16 bytes per 2048 elements and 8
- * per tensor and worker) and synchronises: make lists before a stream capture.  In a context without
+/* Make a list.  With a device, allocates device memory for its tables (16 bytes per 2048 elements, 32
+ * per tensor and 8 per tensor and worker) and synchronises: make lists before a stream capture.  In a context without
  * device the list answers thc_tensors_sizes and thc_tensors_offsets.
  *   tensors  host array of n * count device pointers, worker after worker; NULL is allowed where numel
  *            is 0.  Each is aligned to its element size; contiguous.

@@ -744,7 +744,25 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
     }
 }
 
-// ---------------------------------------------------------------------------------- addresses
+// ---------------------------------------------------------------------------------- tables
+// The pieces of a list, made on the device (a list of 355M elements in 290 tensors: 0.35 ms, with the table from the host 1.6).  `first` is the number of a tensor's first piece; tensors without elements have none.
+struct TensorRow { uint64_t numel, flat; uint32_t first, type; };
+__global__ void list_pieces_kernel(const TensorRow *rows, uint32_t count, Piece *pieces, uint32_t pieces_n)
+{
+    depend_on_previous();
+    const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= pieces_n) return;
+    uint32_t lo = 0, hi = count;                       // the last tensor whose first piece is at most i
+    while (hi - lo > 1u) {
+        const uint32_t mid = lo + (hi - lo) / 2u;
+        if (rows[mid].first <= i) lo = mid;
+        else hi = mid;
+    }
+    const TensorRow r = rows[lo];
+    const uint64_t from = (uint64_t)(i - r.first) * kPiece;
+    pieces[i] = Piece{r.flat + from, lo, (uint32_t)min((uint64_t)kPiece, r.numel - from) | r.type << 16};
+}
+
 constexpr uint32_t kAssignMost = 448;
 struct AssignParams { uint64_t *to; uint32_t n; uint64_t base[kAssignMost]; };
 __global__ void list_assign_kernel(const __grid_constant__ AssignParams P)
@@ -769,8 +787,8 @@ struct thc_tensors {
     struct Range { uint64_t lo, hi; uint32_t index; };
     std::vector<Range> ranges;                 // of the tensors that are not empty, by address
     bool overlapping;                          // tensors of the list overlap each other
+    uint64_t *base;                            // the allocation; pieces are in it
     Piece *pieces;
-    uint64_t *base;
 };
 
 static uint32_t size_of_type(uint32_t t) { return t == THC_F32 ? 4u : 2u; }
@@ -859,18 +877,29 @@ int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uin
         const int rc = take_addresses(h, tensors);
         if (rc != THC_OK) { delete h; return rc; }
         if (view.device >= 0) {
-            std::vector<Piece> pieces;
-            pieces.reserve(pieces_n);
-            for (uint32_t t = 0; t < count; ++t)
-                for (uint64_t e = 0; e < numel[t]; e += kPiece)
-                    pieces.push_back({h->offset[t] + e, t, (uint32_t)std::min<uint64_t>(kPiece, numel[t] - e) | dtype[t] << 16});
-            std::vector<uint64_t> base(h->address.size());
-            for (size_t i = 0; i < base.size(); ++i) base[i] = base_of(h, i);
-            cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&h->pieces), pieces.size() * sizeof(Piece));
-            if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&h->base), base.size() * sizeof(uint64_t));
-            if (e == cudaSuccess) e = cudaMemcpy(h->pieces, pieces.data(), pieces.size() * sizeof(Piece), cudaMemcpyHostToDevice);
-            if (e == cudaSuccess) e = cudaMemcpy(h->base, base.data(), base.size() * sizeof(uint64_t), cudaMemcpyHostToDevice);
-            if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);   // a copy from pageable memory may still be on its way
+            // one allocation: addresses, rows, pieces
+            const size_t base_bytes = h->address.size() * sizeof(uint64_t), rows_bytes = (size_t)count * sizeof(TensorRow);
+            const size_t pieces_at = (base_bytes + rows_bytes + 15) / 16 * 16;
+            std::vector<unsigned char> host(base_bytes + rows_bytes);
+            for (size_t i = 0; i < h->address.size(); ++i) {
+                const uint64_t v = base_of(h, i);
+                memcpy(host.data() + i * sizeof v, &v, sizeof v);
+            }
+            uint32_t first = 0;
+            for (uint32_t t = 0; t < count; ++t) {
+                const TensorRow r{numel[t], h->offset[t], first, dtype[t]};
+                memcpy(host.data() + base_bytes + t * sizeof r, &r, sizeof r);
+                first += (uint32_t)((numel[t] + kPiece - 1) / kPiece);
+            }
+            cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&h->base), pieces_at + (size_t)pieces_n * sizeof(Piece));
+            if (e == cudaSuccess) {
+                h->pieces = reinterpret_cast<Piece *>(reinterpret_cast<char *>(h->base) + pieces_at);
+                e = cudaMemcpy(h->base, host.data(), host.size(), cudaMemcpyHostToDevice);
+            }
+            if (e == cudaSuccess)
+                e = launch_after(list_pieces_kernel, dim3((unsigned)((pieces_n + 255) / 256)), 256, 0, nullptr,
+                                 reinterpret_cast<const TensorRow *>(reinterpret_cast<const char *>(h->base) + base_bytes), count, h->pieces, h->pieces_n);
+            if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
             if (e != cudaSuccess) {
                 thc_tensors_destroy(h);
                 return cuda_fail(e);
@@ -887,7 +916,6 @@ int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uin
 int thc_tensors_destroy(thc_tensors *h)
 {
     if (h == nullptr) return THC_OK;
-    if (h->pieces != nullptr) cudaFree(h->pieces);
     if (h->base != nullptr) cudaFree(h->base);
     delete h;
     return THC_OK;
