@@ -75,19 +75,13 @@ __device__ __forceinline__ uint64_t load_base(const uint64_t *p)
 template <uint32_t T> struct Raw { uint32_t w[T == THC_F32 ? 8 : 4]; };
 template <uint32_t T> __host__ __device__ constexpr uint32_t size_of() { return T == THC_F32 ? 4u : 2u; }
 
-// LAST: nothing reads it again, L2 may drop it first.
-template <uint32_t T, bool LAST = false>
+template <uint32_t T>
 __device__ __forceinline__ Raw<T> load_unit8(uint64_t a)
 {
     Raw<T> r;
-    if constexpr (T == THC_F32 && LAST)
-        asm volatile("ld.global.L2::evict_first.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(a));
-    else if constexpr (T == THC_F32)
+    if constexpr (T == THC_F32)
         asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(a));
-    else if constexpr (LAST)
-        asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(a));
     else
         asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(a));
     return r;
@@ -171,7 +165,7 @@ constexpr uint32_t kNotHeld = 0xFFFFFFFFu;
 // ---------------------------------------------------------------------------------- norm
 // s + the squares of a unit.  fp32: each square in fp64, which no value leaves.  16 bits: the squares are exact in fp32, eight
 // of them are added there in three levels (3 x 2^-24 off at most, as all are positive) and the sum in fp64: a conversion and an fp64
-// operation per unit instead of eight, which were what bounded it (355M bf16: 125 us, now 111).  fp16's squares and their sums
+// operation per unit instead of eight, which were what bounded it (355M bf16: 125 us, now 110 to 117).  fp16's squares and their sums
 // stay within fp32; for bf16 a sum outside [2^-100, 2^126] (a square may have left fp32's range) is formed as for fp32.
 template <uint32_t T>
 __device__ __forceinline__ void add_squares(double (&s)[2], const Raw<T> &r)
@@ -425,7 +419,7 @@ __device__ __forceinline__ void adam_item(const AdamPlace &a, const AdamStep &k,
 }
 
 // ---------------------------------------------------------------------------------- the calls
-enum ClipKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter, kAdam, kAdamMaster };
+enum ClipKind { kClip, kGatherF32, kGatherBf16, kGatherResidual, kScatter, kAdam, kAdamMaster, kNorm };
 __host__ __device__ constexpr bool is_adam(ClipKind k) { return k == kAdam || k == kAdamMaster; }
 // CTAs of list_product_kernel on an SM, by registers.  us with 2, 3, 4: 8 x 25.6M fp32 gathered 243, 242, 249; 355M scattered to
 // bf16 306, 305, 312; 138M bf16 clipped -, 141, 135; Adam step of 138M (two units at a time only with 2) 735, 806, -.
@@ -695,11 +689,11 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
     for (; c < items; c += stride) {
         last = p;
         if (c + stride < items) p = load_item(P.L, c + stride, P.split_log2);
-        else last_base = load_item_base<K>(P, last, worker);
-        s += squares<true>(last, base, P.src_flat, lane, c + stride < items ? kNotHeld : held);
+        else if (K != kNorm) last_base = load_item_base<K>(P, last, worker);
+        s += squares<K != kNorm>(last, base, P.src_flat, lane, K == kNorm || c + stride < items ? kNotHeld : held);
     }
     Early<K> early{};
-    if (first < items) early = load_early<K>(P, last, last_base, lane, held);
+    if (K != kNorm && first < items) early = load_early<K>(P, last, last_base, lane, held);
     const double sum = sum_of_cta(s, red);
     __syncwarp();
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");             // all CTAs run
@@ -725,27 +719,29 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
             else if (is_adam(K)) *P.adam.step = t;     // every CTA has read it before the barrier
         }
     }
-    __syncthreads();
-    if (is_adam(K)) {
-        if (s_result.stop != 0u) return;
-        k.step_size = s_result.step_size;
-        k.inv_sqrt_by2 = s_result.inv_sqrt_by2;
-    }
-    k.c = s_result.c;
-    if (first >= items) return;
-    const uint32_t final = first + (items - 1u - first) / stride * stride;
-    products<K>(P, last, last_base, early, worker, k, lr, lane, held);
+    if constexpr (K != kNorm) {
+        __syncthreads();
+        if (is_adam(K)) {
+            if (s_result.stop != 0u) return;
+            k.step_size = s_result.step_size;
+            k.inv_sqrt_by2 = s_result.inv_sqrt_by2;
+        }
+        k.c = s_result.c;
+        if (first >= items) return;
+        products<K>(P, last, last_base, early, worker, k, lr, lane, held);
 #pragma unroll 1
-    for (c = final; c >= stride; ) {
-        c -= stride;
-        p = load_item(P.L, c, P.split_log2);
-        last_base = load_item_base<K>(P, p, worker);
-        products<K>(P, p, last_base, load_early<K>(P, p, last_base, lane, kNotHeld), worker, k, lr, lane, kNotHeld);
+        for (c = first + (items - 1u - first) / stride * stride; c >= stride;) {
+            c -= stride;
+            p = load_item(P.L, c, P.split_log2);
+            last_base = load_item_base<K>(P, p, worker);
+            products<K>(P, p, last_base, load_early<K>(P, p, last_base, lane, kNotHeld), worker, k, lr, lane, kNotHeld);
+        }
     }
 }
 
 // ---------------------------------------------------------------------------------- tables
-// The pieces of a list, made on the device (a list of 355M elements in 290 tensors: 0.35 ms, with the table from the host 1.6).  `first` is the number of a tensor's first piece; tensors without elements have none.
+// The pieces of a list, made on the device (a list of 355M elements in 290 tensors: 0.35 ms, with the table from the host 1.6).
+// `first` is the number of a tensor's first piece; tensors without elements have none.
 struct TensorRow { uint64_t numel, flat; uint32_t first, type; };
 __global__ void list_pieces_kernel(const TensorRow *rows, uint32_t count, Piece *pieces, uint32_t pieces_n)
 {
@@ -1058,25 +1054,41 @@ static int launch_norm(ListParams &P, const thc_tensors *h, bool alone, cudaStre
     return THC_OK;
 }
 
-int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes, void *stream)
-{
-    int rc = check_list(ctx, list);
-    if (rc != THC_OK) return rc;
-    if (norms == nullptr || !aligned4(norms)) return THC_EINVAL;
-    if ((rc = check_workspace(list, workspace, workspace_bytes)) != THC_OK) return rc;
-    ListParams P;
-    memset(&P, 0, sizeof P);
-    fill_params(P, ctx, list, INFINITY, norms, workspace);
-    P.result = nullptr;
-    return launch_norm<false>(P, list, true, static_cast<cudaStream_t>(stream));
-}
-
 // Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
 //   pieces          16          32          48          64          96
 //   gather       4.3 / 6.0   4.6 / 5.6   5.2 / 5.6   5.3 / 5.7   8.3 / 5.8
 //   Adam step    6.2 / 6.7   7.8 / 6.7  10.1 / 7.2  10.3 / 7.3  17.0 / 7.8
 static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 16u : 64u; }
 
+template <ClipKind K>
+static int launch_cluster(ParamsOf<K> &P, const thc_tensors *h, cudaStream_t st)
+{
+    P.split_log2 = std::max(1u, split_of(h, kClusterCtas * kClusterWarps));   // (1: see kHeldBytes)
+    const size_t smem = K == kNorm ? 0 : kHeldBytes * kClusterWarps;
+    if (smem != 0) {
+        const int rc = ensure_dynamic_smem(reinterpret_cast<const void *>(list_cluster_kernel<K>));
+        if (rc != THC_OK) return rc;
+    }
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kClusterCtas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(kClusterCtas, h->n);
+    cfg.blockDim = dim3(kClusterThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    THC_CUDA(cudaLaunchKernelEx(&cfg, list_cluster_kernel<K>, P));
+    return THC_OK;
+}
+
+// Up to so many pieces over all workers the products' warps add the sums themselves, which leaves out the last CTA's turn.  us,
+// so / by the last CTA: 1024 pieces of bf16 gathered 7.4 / 8.1, 4096 13.5 / 14.1; beyond them too many warps would.
 constexpr uint32_t kOwnSumsMostPieces = 4096;
 
 template <ClipKind K>
@@ -1084,28 +1096,7 @@ static int launch_call(ParamsOf<K> &P, const thc_ctx *ctx, const thc_tensors *h,
 {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     fill_params(P, ctx, h, max_norm, norms, workspace);
-    if (norms != nullptr && h->pieces_n <= cluster_most_pieces(K)) {
-        P.split_log2 = std::max(1u, split_of(h, kClusterCtas * kClusterWarps));   // (1: see kHeldBytes)
-        const void *kern = reinterpret_cast<const void *>(list_cluster_kernel<K>);
-        const int rc = ensure_dynamic_smem(kern);
-        if (rc != THC_OK) return rc;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = kClusterCtas;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof cfg);
-        cfg.gridDim = dim3(kClusterCtas, h->n);
-        cfg.blockDim = dim3(kClusterThreads);
-        cfg.dynamicSmemBytes = kHeldBytes * kClusterWarps;
-        cfg.stream = st;
-        cfg.attrs = attr;
-        cfg.numAttrs = 2;
-        THC_CUDA(cudaLaunchKernelEx(&cfg, list_cluster_kernel<K>, P));
-        return THC_OK;
-    }
+    if (norms != nullptr && h->pieces_n <= cluster_most_pieces(K)) return launch_cluster<K>(P, h, st);
     if (norms != nullptr) {
         if ((uint64_t)h->pieces_n * h->n <= kOwnSumsMostPieces) P.partials = norm_shape(h, split_of_norm(h), false).ctas;
         const int rc = launch_norm<is_adam(K)>(P, h, false, st);
@@ -1115,6 +1106,21 @@ static int launch_call(ParamsOf<K> &P, const thc_ctx *ctx, const thc_tensors *h,
     const uint64_t items = ((uint64_t)h->pieces_n << P.split_log2) * h->n;
     THC_CUDA(launch_after(list_product_kernel<K>, dim3((unsigned)((items + kListWarps - 1) / kListWarps)), kListThreads, 0, st, P));
     return THC_OK;
+}
+
+int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    if (norms == nullptr || !aligned4(norms)) return THC_EINVAL;
+    if ((rc = check_workspace(list, workspace, workspace_bytes)) != THC_OK) return rc;
+    ListParams P;
+    memset(&P, 0, sizeof P);
+    fill_params(P, ctx, list, INFINITY, norms, workspace);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (list->pieces_n <= cluster_most_pieces(kNorm)) return launch_cluster<kNorm>(P, list, st);
+    P.result = nullptr;
+    return launch_norm<false>(P, list, true, st);
 }
 
 // max_norm, norms and workspace of a call that clips.

@@ -127,6 +127,8 @@ for n in (1, 4):
     h = lst([64 * 2048], [0], n)
     assert call("thc_gather_grads", h, 1.0, None, fl, N) == 0
     assert rows() == [("cluster_", [8, 512, 65536, 8])]
+    assert call("thc_grad_norm", h, N) == 0
+    assert rows() == [("cluster_", [8, 512, 0, 8])]
     h = lst([64 * 2048, 1], [0, 0], n)
     assert call("thc_gather_grads", h, 1.0, None, fl, N) == 0
     got = rows()
