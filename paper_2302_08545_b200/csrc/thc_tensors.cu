@@ -1141,12 +1141,13 @@ int thc_clip_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const
     if ((rc = check_clip(list, max_norm, norms, true, workspace, workspace_bytes)) != THC_OK) return rc;
     if (out->n != list->n || out->numel != list->numel || out->dtype != list->dtype || out->overlapping) return THC_EINVAL;
     if (out != list) {
+        // both sorted by address; those of `out` do not overlap each other
+        size_t j = 0;
         for (const auto &r : list->ranges) {
-            if (out->address[r.index] == r.lo) {
-                // its own place, and as tensors of `out` do not overlap each other, no other one's
-                continue;
-            }
-            if (overlaps(out, r.lo, r.hi)) return THC_EINVAL;
+            while (j < out->ranges.size() && out->ranges[j].hi <= r.lo) ++j;
+            if (j == out->ranges.size()) break;
+            const auto &w = out->ranges[j];
+            if (w.lo < r.hi && !(w.lo == r.lo && w.index == r.index)) return THC_EINVAL;
         }
     }
     ListParams P;

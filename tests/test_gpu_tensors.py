@@ -130,10 +130,15 @@ def test_max_norm_zero_and_zero_gradients():
     assert float(norms) == 0.0 and all(not bool(x.any()) for x in workers[0]) and ctx.status() == 0
 
 
+# lists that take the cluster, sums that the products add themselves, sums that the last CTA adds
+LENGTHS = [[100, 5000], [100, 700_000], [100, 5_000_000]]
+
+
+@pytest.mark.parametrize("sizes", LENGTHS)
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
-def test_values_that_are_not_finite(value):
+def test_values_that_are_not_finite(value, sizes):
     from paper_2302_08545_b200 import thc
-    workers = T.make([100, 5000], ["f32", "bf16"], 3, seed=4)
+    workers = T.make(sizes, ["f32", "bf16"], 3, seed=4)
     workers[1][1][4321] = value
     old = [[x.clone() for x in w] for w in workers]
     ctx, lst, norms, ws = setup(workers)
@@ -325,9 +330,10 @@ def test_adamw(sizes, types, shift, master, per_tensor):
             assert torch.equal(y[~inside], o[~inside])
 
 
-def test_adamw_skips_a_step_whose_norm_is_not_finite():
+@pytest.mark.parametrize("size", [5000, 700_000, 9_000_001])
+def test_adamw_skips_a_step_whose_norm_is_not_finite(size):
     from paper_2302_08545_b200 import thc
-    workers = T.make([5000, 10], ["bf16"], 1)
+    workers = T.make([size, 10], ["bf16"], 1)
     ctx, lst, norms, ws = setup(workers)
     grad = torch.randn(lst.d, device="cuda")
     grad[lst.offsets[1] - 1] = math.nan    # between the tensors: does not matter
@@ -469,6 +475,35 @@ def test_refused_arguments():
         ctx.clip_grads(one, 1.0, norms, ws, out=half)
     assert code(lambda: ctx.grad_norm(half, norms, ws)) == EINVAL
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("at", [4, 8])
+@pytest.mark.parametrize("sizes", [[5000, 33], [300_001, 33]])
+def test_vectors_that_start_at_16_bytes(sizes, at):
+    """16 bytes are what the calls ask for; units of fp32 are 32."""
+    from paper_2302_08545_b200 import thc
+    workers = T.make(sizes, ["bf16", "f32"], 1, seed=3)
+    ctx, lst, norms, ws = setup(workers)
+    vectors = [torch.rand(lst.d + 8, device="cuda")[at: at + lst.d] for _ in range(6)]
+    g, m, v, w, x, e = vectors
+    e0 = e.double()
+    ctx.gather_grads(lst, 10.0, [x], norms, ws, ef=[e])
+    r, = check_norms(norms, workers)
+    for t, y, z in zip(workers[0], lst.views(x), lst.views(e0)):
+        product = t.double() * T.factor(r, 10.0)
+        T.within(y, product + z, (product.abs() * 2.5 * U + (product + z).abs() * U) * SMALL + 2.0 ** -149)
+    m0, v0, w0 = m.double(), v.double(), w.double()
+    lr, step = torch.full((1,), 1e-2, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    ctx.adamw(g, lst, lr, step, m, v, norms, ws, master=w, betas=(0.9, 0.99), eps=1e-6, max_norm=1.0)
+    r, = check_norms(norms, [lst.views(g)])
+    for i, t in enumerate(workers[0]):
+        m2, v2, w2, dm, dv, dw = adam_exact(*(lst.views(y)[i] for y in (g.double(), m0, v0, w0)), T.factor(r, 1.0), 1, float(lr), 0.0, 0.9, 0.99, 1e-6)
+        T.within(lst.views(m)[i], m2, dm)
+        T.within(lst.views(v)[i], v2, dv)
+        T.within(lst.views(w)[i], w2, dw)
+        assert torch.equal(t, lst.views(w)[i].to(t.dtype))
+    ctx.scatter_grads(w, math.inf, lst, None, None)
+    assert all(torch.equal(t, y.to(t.dtype)) for t, y in zip(workers[0], lst.views(w)))
 
 
 def test_positions_past_32_bits():

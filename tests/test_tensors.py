@@ -170,6 +170,19 @@ assert call("thc_clip_grads", h, 1.0, lst([100, 70], [0, 0], at=(1 << 33) + 4), 
 assert call("thc_clip_grads", h, 1.0, lst([100, 70], [0, 0], at=(1 << 33) + (1 << 30), step=-(1 << 30)), N) == E
 twice = lst([100, 70], [0, 0], step=0)
 assert call("thc_grad_norm", twice, N) == 0 and call("thc_clip_grads", twice, 1.0, None, N) == E
+g3 = lst([100, 70, 9], [0, 0, 0], at=1 << 42)
+def create(places):
+    h, k = ctypes.c_void_p(), 3
+    rc = L.thc_tensors_create(c._h, p(*[(1 << 42) + v for v in places]), (ctypes.c_uint64 * k)(100, 70, 9), (ctypes.c_uint32 * k)(0, 0, 0), 1, k, ctypes.byref(h))
+    assert rc == 0
+    return h
+G = 1 << 30
+assert call("thc_clip_grads", g3, 1.0, create((0, 5 * G, 2 * G)), N) == 0          # two of them in place
+assert call("thc_clip_grads", g3, 1.0, create((5 * G, 6 * G, 7 * G)), N) == 0      # none
+assert call("thc_clip_grads", g3, 1.0, create((0, G, 2 * G + 4)), N) == E          # the last one beside its place
+assert call("thc_clip_grads", g3, 1.0, create((0, 2 * G, 5 * G)), N) == E          # one over another
+assert call("thc_clip_grads", g3, 1.0, create((5 * G, G - 4, 6 * G)), N) == E
+assert call("thc_clip_grads", g3, 1.0, create((400, G, 2 * G)), N) == 0            # right behind the tensor
 log()
 assert call("thc_gather_grads", h, 1.0, None, p(F[0]), None) == E          # a bound needs the norm
 assert call("thc_gather_grads", h, 1.0, None, None, N) == E and call("thc_gather_grads", h, 1.0, None, p(None), N) == E
