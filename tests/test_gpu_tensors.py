@@ -586,3 +586,33 @@ def test_many_calls_in_a_row_of_every_length():
         T.within(norms[0, i, : lst.n].cpu(), ref, ref * 2.6 * U)
         assert bool((norms[:, i] == norms[0, i]).all())
     assert ctx.status() == 0
+
+
+def test_two_contexts_on_two_streams():
+    """The same list at the same time from two contexts, each with a stream and a workspace of its own; the stream given, or the
+    current one."""
+    from paper_2302_08545_b200 import thc
+    for sizes in ([3000, 70], [2_000_003, 70], [9_000_001, 5]):
+        workers = T.make(sizes, ["f32", "bf16"], 1, seed=6)
+        first, second = context(), context()
+        lst = thc.Tensors(first, workers)
+        calls = []
+        for ctx in (first, second):
+            stream = torch.cuda.Stream()
+            calls.append((ctx, stream, torch.empty(lst.workspace_bytes, dtype=torch.uint8, device="cuda"), torch.zeros(30, 1, device="cuda"),
+                          torch.empty(lst.d, device="cuda")))
+        torch.cuda.synchronize()
+        for r in range(30):
+            for i, (ctx, stream, ws, norms, flat) in enumerate(calls):
+                if i == 0:
+                    ctx.gather_grads(lst, 1.0 + i, [flat], norms[r], ws, stream=stream)
+                else:
+                    with torch.cuda.stream(stream):
+                        ctx.gather_grads(lst, 1.0 + i, [flat], norms[r], ws)
+        torch.cuda.synchronize()
+        for i, (ctx, stream, ws, norms, flat) in enumerate(calls):
+            r, = check_norms(norms[0], workers)
+            assert bool((norms == norms[0]).all()) and ctx.status() == 0
+            for x, y in zip(workers[0], lst.views(flat)):
+                exact = x.double() * T.factor(r, 1.0 + i)
+                T.within(y, exact, exact.abs() * (before(workers) + 2 * U) * SMALL + 2.0 ** -149)
