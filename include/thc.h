@@ -316,9 +316,10 @@ int thc_tensors_offsets(const thc_tensors *list, uint64_t *offsets);
  * that were given at capture, which the checks of later calls do not know of). */
 int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *list, const void *const *tensors, void *stream);
 
-/* Global L2 norm of each worker's tensors: norms[i] = sqrt(sum over all tensors of worker i of x^2), squares
- * summed in fp64 in a fixed order (the same bits on every call).  A tensor that stands in the list twice
- * counts twice.  A norm that is NaN or infinite sets THC_STATUS_NONFINITE.
+/* Global L2 norm of each worker's tensors: norms[i] = sqrt(sum over all tensors of worker i of x^2).  Squares of
+ * fp32 are summed in fp64, those of 16-bit types eight at a time in fp32 (which moves the norm by at most
+ * 1.5 x 2^-24 of it) and then in fp64, in a fixed order (the same bits on every call).  A tensor that stands in the list
+ * twice counts twice.  A norm that is NaN or infinite sets THC_STATUS_NONFINITE.
  *   norms  device, n fp32, written (4-byte aligned, here and below)                              */
 int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes,
                   void *stream);

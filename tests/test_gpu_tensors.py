@@ -616,3 +616,28 @@ def test_two_contexts_on_two_streams():
             for x, y in zip(workers[0], lst.views(flat)):
                 exact = x.double() * T.factor(r, 1.0 + i)
                 T.within(y, exact, exact.abs() * (before(workers) + 2 * U) * SMALL + 2.0 ** -149)
+
+
+def test_twenty_thousand_tensors():
+    """More tensors than CTAs, most of them shorter than a unit or empty, pieces of one allocation in an order of their own."""
+    from paper_2302_08545_b200 import thc
+    n = 20_000
+    sizes = [(7 * i) % 40 if i % 5 else 0 for i in range(n)]
+    sizes[12_345] = 100_000
+    ends = torch.tensor(sizes).cumsum(0).tolist()
+    room = torch.randn(ends[-1], device="cuda")
+    order = sorted(range(n), key=lambda i: (i * 7919) % n)
+    pieces = [room[ends[i] - sizes[i]: ends[i]] for i in order]
+    ctx, lst, norms, ws = setup([pieces])
+    flat = torch.full((lst.d,), 5.0, device="cuda")
+    ctx.gather_grads(lst, math.inf, [flat], norms, ws)
+    check_norms(norms, [[room]])
+    joined = torch.cat(pieces)
+    places = torch.cat([torch.arange(o, o + p.numel()) for o, p in zip(lst.offsets, pieces)]).cuda()
+    assert torch.equal(flat[places], joined)
+    flat[places] = 0.0
+    assert not bool(flat.any())
+    moved = torch.randn_like(room)
+    lst.assign([[moved[p.storage_offset(): p.storage_offset() + p.numel()] for p in pieces]])
+    ctx.clip_grads(lst, 1.0, norms, ws)
+    assert abs(float(torch.linalg.vector_norm(moved.double())) - 1.0) < 1e-5
