@@ -303,7 +303,8 @@ typedef struct thc_tensors_sizes_t {
  *   numel    host array of `count` sizes, at least one above 0, 2^40 in all at most
  *   dtype    host array of `count` THC_F32 / THC_BF16 / THC_F16
  *   n        1..THC_MAX_WORKERS;  count  1..2^20
- * thc_tensors_destroy synchronises the device (cudaFree). */
+ * thc_tensors_destroy synchronises the device (cudaFree).  A captured call reads the list's tables when it is
+ * replayed: destroy the list after the graph. */
 int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uint64_t *numel, const uint32_t *dtype,
                        uint32_t n, uint32_t count, thc_tensors **list);
 int thc_tensors_destroy(thc_tensors *list);

@@ -656,6 +656,7 @@ list_product_kernel(const __grid_constant__ ParamsOf<K> P)
 
 // Both in one launch, grid (8 CTAs, workers), a cluster per worker.  The CTAs' sums are written to all CTAs' shared memory;
 // each adds them in the same order and forms norm and factor itself.  A warp's last item is still in its shared memory.
+// A chain of latencies: 4 x 65,536 fp32 gathered in 5.0 us, of which an empty launch of clusters is 2.1.
 template <ClipKind K>
 __global__ void __launch_bounds__(kClusterThreads, 1)
 list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
@@ -912,7 +913,13 @@ int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uin
 int thc_tensors_destroy(thc_tensors *h)
 {
     if (h == nullptr) return THC_OK;
-    if (h->base != nullptr) cudaFree(h->base);
+    if (h->base != nullptr) {
+        // (a list may be collected while its thread captures a graph, which a plain cudaFree would spoil)
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        const bool relaxed = cudaThreadExchangeStreamCaptureMode(&mode) == cudaSuccess;
+        cudaFree(h->base);
+        if (relaxed) cudaThreadExchangeStreamCaptureMode(&mode);
+    }
     delete h;
     return THC_OK;
 }

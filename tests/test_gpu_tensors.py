@@ -641,3 +641,22 @@ def test_twenty_thousand_tensors():
     lst.assign([[moved[p.storage_offset(): p.storage_offset() + p.numel()] for p in pieces]])
     ctx.clip_grads(lst, 1.0, norms, ws)
     assert abs(float(torch.linalg.vector_norm(moved.double())) - 1.0) < 1e-5
+
+
+def test_a_list_that_goes_during_a_capture():
+    """Destroying one list does not spoil a capture of calls on another."""
+    from paper_2302_08545_b200 import thc
+    workers = T.make([5000, 64], ["f32"], 1, seed=3)
+    ctx, lst, norms, ws = setup(workers)
+    other = thc.Tensors(ctx, T.make([100], ["f32"], 1))
+    ctx.grad_norm(lst, norms, ws)
+    norms.zero_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.grad_norm(lst, norms, ws)
+        other.close()
+        ctx.grad_norm(lst, norms, ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    check_norms(norms, workers)
