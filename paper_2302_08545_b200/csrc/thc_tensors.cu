@@ -165,8 +165,9 @@ constexpr uint32_t kNotHeld = 0xFFFFFFFFu;
 // ---------------------------------------------------------------------------------- norm
 // s + the squares of a unit.  fp32: each square in fp64, which no value leaves.  16 bits: the squares are exact in fp32, eight
 // of them are added there in three levels (3 x 2^-24 off at most, as all are positive) and the sum in fp64: a conversion and an fp64
-// operation per unit instead of eight, which were what bounded it (355M bf16: 125 us, now 110 to 117).  fp16's squares and their sums
-// stay within fp32; for bf16 a sum outside [2^-100, 2^126] (a square may have left fp32's range) is formed as for fp32.
+// operation per unit instead of eight, which were what bounded it (355M bf16: 125 us, now 106).  fp16's squares and their sums
+// stay within fp32; for bf16 a sum outside [2^-100, 2^126] (a square may have left fp32's range) is formed as for fp32, in a loop
+// (unrolled it takes the registers of the ordinary case: 111 us).
 template <uint32_t T>
 __device__ __forceinline__ void add_squares(double (&s)[2], const Raw<T> &r)
 {
@@ -180,6 +181,14 @@ __device__ __forceinline__ void add_squares(double (&s)[2], const Raw<T> &r)
             return;
         }
         if (((r.w[0] | r.w[1] | r.w[2] | r.w[3]) & 0x7FFF7FFFu) == 0u) return;
+#pragma unroll 1
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t w = e == 0 ? r.w[0] : e == 1 ? r.w[1] : e == 2 ? r.w[2] : r.w[3];
+            const double lo = (double)__uint_as_float(w << 16), hi = (double)__uint_as_float(w & 0xFFFF0000u);
+            s[0] = fma(lo, lo, s[0]);
+            s[1] = fma(hi, hi, s[1]);
+        }
+        return;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -192,7 +201,7 @@ __device__ __forceinline__ void add_squares(double (&s)[2], const Raw<T> &r)
 template <uint32_t T, bool HOLD>
 __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uint32_t lane, uint32_t held)
 {
-    constexpr int kBatch = T == THC_F32 ? 4 : 8;
+    constexpr int kBatch = 4;
     double s[2] = {0.0, 0.0};
     const uint32_t head = min(head_of<T>(a), len), units = (len - head) / kUnit, tail = head + units * kUnit;
     // lanes 0..7 the elements before the units, lanes 8..15 those behind
@@ -225,14 +234,13 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
     return fma(v, v, s[0]) + s[1];
 }
 
-// ONLY32: nothing but fp32 is read.
-template <bool HOLD, bool ONLY32 = false>
+template <bool HOLD>
 __device__ __forceinline__ double squares(const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane, uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu, type = p.len_type >> 16;
     if (flat != 0) return squares_of_piece<THC_F32, HOLD>(flat + p.flat * 4u, len, lane, held);
     const uint64_t b = load_base(base + p.tensor);
-    if (ONLY32 || type == THC_F32) return squares_of_piece<THC_F32, HOLD>(b + p.flat * 4u, len, lane, held);
+    if (type == THC_F32) return squares_of_piece<THC_F32, HOLD>(b + p.flat * 4u, len, lane, held);
     if (type == THC_BF16) return squares_of_piece<THC_BF16, HOLD>(b + p.flat * 2u, len, lane, held);
     return squares_of_piece<THC_F16, HOLD>(b + p.flat * 2u, len, lane, held);
 }
@@ -546,10 +554,8 @@ __device__ __forceinline__ float adam_inv_sqrt(const AdamParams &a, int64_t t) {
 // time, go side by side through `rounds` rounds of pieces, the next row of CTAs through the next rounds.  (One row for all of
 // it drifts apart, which DRAM minds while the last launch's writes still leave L2: 355M scattered 526 us, in eight rows 507;
 // eight workers gathered 380, 366.)  The sums are added in a fixed order; a worker's last CTA does that and forms what the products
-// need (ADAM: also the step count, unless the norm is not finite), or the products' warps do.  ONLY32: the same with nothing but
-// fp32 to read (with the code for 16 bits beside it the registers do not suffice, and eight workers' 25.6M fp32 take 135 us
-// instead of 117).
-template <bool ADAM, bool ONLY32>
+// need (ADAM: also the step count, unless the norm is not finite), or the products' warps do.
+template <bool ADAM>
 __global__ void __launch_bounds__(kListThreads, kNormCtasPerSm)
 list_norm_kernel(const __grid_constant__ ListParams P)
 {
@@ -567,7 +573,7 @@ list_norm_kernel(const __grid_constant__ ListParams P)
         const Piece now = p;
         c += stride;
         if (c < end) p = load_item(P.L, c, P.split_log2);
-        s += squares<false, ONLY32>(now, base, P.src_flat, lane, kNotHeld);
+        s += squares<false>(now, base, P.src_flat, lane, kNotHeld);
     }
     __shared__ double red[kListWarps];
     __shared__ NormResult s_result;
@@ -925,7 +931,7 @@ int thc_tensors_destroy(thc_tensors *h)
 }
 
 // CTAs per worker of the sums: rows of as many as run at a time (see list_norm_kernel), each of them at least six rounds long; one
-// row where nothing is written after them (355M bf16, us: 112, in six rows 117; fp32 of the same bytes 103, 105).
+// row where nothing is written after them, which is then 2 to 5 % faster.
 struct NormShape { uint32_t row, rounds, ctas; };
 static NormShape norm_shape(const thc_tensors *h, uint32_t split_log2, bool alone)
 {
@@ -1056,8 +1062,7 @@ static int launch_norm(ListParams &P, const thc_tensors *h, bool alone, cudaStre
     P.row = shape.row;
     P.rounds = shape.rounds;
     const dim3 grid(shape.ctas, h->n);
-    if (ADAM || P.src_flat != 0 || h->all_f32) THC_CUDA(launch_after(list_norm_kernel<ADAM, true>, grid, kListThreads, 0, st, static_cast<const ListParams &>(P)));
-    else THC_CUDA(launch_after(list_norm_kernel<false, false>, grid, kListThreads, 0, st, P));
+    THC_CUDA(launch_after(list_norm_kernel<ADAM>, grid, kListThreads, 0, st, static_cast<const ListParams &>(P)));
     return THC_OK;
 }
 
