@@ -344,6 +344,21 @@ int thc_clip_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const
 int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *const *ef_or_null,
                      void *const *flats, float *norms, void *workspace, uint64_t workspace_bytes, void *stream);
 
+/* A round with a gradient that is not finite is void.  Its blocks have scale 0 (see thc_prepare) where one GPU has all the gradients,
+ * and indices that stand for nothing where another rank's scale counts, so the average is finite and wrong.  This call stands behind
+ * the one that writes the average and before thc_error_feedback.  If any of `norms` (what thc_gather_grads wrote; across
+ * ranks their sum over all ranks) is NaN or infinite,
+ *     out[j] = NaN,   scales = 0,   grads[i] = ef[i],
+ * and THC_STATUS_NONFINITE is set: thc_error_feedback then leaves each residual as it was, thc_adamw takes no step and
+ * thc_scatter_grads hands the NaN on.  Otherwise nothing is written.  A norm that fp32 does not hold (it reads infinity) counts as infinite.
+ *   list        the gradients that were gathered
+ *   norms       device, n fp32, read
+ *   scales      device, thc_sizes_t.scales_count fp32 of the list's d;   out  device, sizes.d fp32
+ *   grads, ef   host arrays of n device pointers as in thc_error_feedback, all apart from each other (THC_EINVAL); both
+ *               NULL without residuals (fp32 contexts only, THC_EUNSUPPORTED otherwise)                     */
+int thc_void_round(thc_ctx *ctx, const thc_tensors *list, const float *norms, float *scales, float *out,
+                   float *const *grads_or_null, const float *const *ef_or_null, void *stream);
+
 /* The way out of a round: the flat average that thc_decompress wrote, clipped by the norm of what belongs to
  * tensors (its noise between them does not count), to the tensors of a list with n = 1, each in its type.
  *   flat   device, sizes.d fp32, read; a tensor of the list may be its own place in it

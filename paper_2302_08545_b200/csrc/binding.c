@@ -449,6 +449,24 @@ static PyObject *b_gather_grads(ARGS)
     CALL(thc_gather_grads(ctx, list, most, (const float *const *)array_of(&e), array_of(&f), norms, ws, wb, st));
 }
 
+/* (handle, list, norms, scales, out, grads, ef, stream) */
+static PyObject *b_void_round(ARGS)
+{
+    void *ctx_p, *st, *norms, *scales, *out;
+    thc_tensors *list;
+    thc_tensors_sizes_t sz;
+    thc_sizes_t round;
+    list_t g, e;
+    int rc;
+    (void)self;
+    if (want(na, 8) || address(a[0], &ctx_p) || list_of(a[1], &list, &sz) || list_stream(a[7], &sz, &st)) return NULL;
+    memset(&round, 0, sizeof round);
+    if (ctx_p != NULL && sz.n != 0) thc_sizes(ctx_p, sz.d, 1, &round);
+    if (vector(a[2], &norms, F32, sz.n, &sz, "norms") || vector(a[3], &scales, F32, round.scales_count, &sz, "scales") ||
+        vector(a[4], &out, F32, sz.d, &sz, "out") || vectors(a[5], &g, F32, &sz, "grads") || vectors(a[6], &e, F32, &sz, "ef")) return NULL;
+    CALL(thc_void_round(ctx_p, list, norms, scales, out, (rot_t)array_of(&g), (const float *const *)array_of(&e), st));
+}
+
 /* (handle, flat, max_norm, list, norms, workspace, stream) */
 static PyObject *b_scatter_grads(ARGS)
 {
@@ -479,7 +497,7 @@ static PyMethodDef methods[] = {
     ENTRY(prepare), ENTRY(prepare_minmax), ENTRY(compress), ENTRY(prepare_compress), ENTRY(quantize_rotated),
     ENTRY(aggregate), ENTRY(decompress), ENTRY(aggregate_decompress), ENTRY(error_feedback),
     ENTRY(accumulate_error), ENTRY(prepare_noalloc), ENTRY(grad_norm), ENTRY(clip_grads), ENTRY(gather_grads),
-    ENTRY(scatter_grads), ENTRY(adamw), {NULL, NULL, 0, NULL}};
+    ENTRY(void_round), ENTRY(scatter_grads), ENTRY(adamw), {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

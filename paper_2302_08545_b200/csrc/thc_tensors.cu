@@ -746,6 +746,36 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
     }
 }
 
+// ---------------------------------------------------------------------------------- void rounds
+struct VoidParams {
+    const float *norms;
+    float *scales, *out;
+    uint64_t d, scales_n;
+    uint32_t n, residuals;       // residuals: n or 0
+    DeviceBlock *dev;
+    float *grads[THC_MAX_WORKERS];
+    const float *ef[THC_MAX_WORKERS];
+};
+
+// Writes what a void round leaves (see thc.h), or, as nearly always, reads n numbers and ends.  d is a multiple of 64, every vector aligned
+// to 16 bytes.
+__global__ void __launch_bounds__(kListThreads)
+void_round_kernel(const __grid_constant__ VoidParams P)
+{
+    depend_on_previous();
+    const bool bad = threadIdx.x < P.n && !isfinite(ld_global(P.norms + threadIdx.x));
+    if (!__syncthreads_or(bad)) return;
+    const uint64_t first = (uint64_t)blockIdx.x * kListThreads + threadIdx.x, stride = (uint64_t)gridDim.x * kListThreads;
+    const float nan = __uint_as_float(0x7FFFFFFFu);
+    for (uint64_t j = first; j < P.d / 4u; j += stride) {
+        reinterpret_cast<float4 *>(P.out)[j] = make_float4(nan, nan, nan, nan);
+        for (uint32_t i = 0; i < P.residuals; ++i)
+            reinterpret_cast<uint4 *>(P.grads[i])[j] = ld_global(reinterpret_cast<const uint4 *>(P.ef[i]) + j);
+    }
+    for (uint64_t j = first; j < P.scales_n; j += stride) P.scales[j] = 0.0f;
+    if (first == 0) atomicOr(&P.dev->status, THC_STATUS_NONFINITE);
+}
+
 // ---------------------------------------------------------------------------------- tables
 // The pieces of a list, made on the device (a list of 355M elements in 290 tensors: 0.35 ms, with the table from the host 1.6).
 // `first` is the number of a tensor's first piece; tensors without elements have none.
@@ -1199,6 +1229,51 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
     if (ef_or_null != nullptr) return launch_call<kGatherResidual>(P, ctx, list, max_norm, norms, workspace, stream);
     if (bf16) return launch_call<kGatherBf16>(P, ctx, list, max_norm, norms, workspace, stream);
     return launch_call<kGatherF32>(P, ctx, list, max_norm, norms, workspace, stream);
+}
+
+int thc_void_round(thc_ctx *ctx, const thc_tensors *list, const float *norms, float *scales, float *out, float *const *grads_or_null,
+                   const float *const *ef_or_null, void *stream)
+{
+    int rc = check_list(ctx, list);
+    if (rc != THC_OK) return rc;
+    if (norms == nullptr || !aligned4(norms) || scales == nullptr || !aligned16(scales) || out == nullptr || !aligned16(out)) return THC_EINVAL;
+    if ((grads_or_null == nullptr) != (ef_or_null == nullptr)) return THC_EINVAL;
+    if (ef_or_null != nullptr && view_of(ctx).in_dtype != THC_F32) return THC_EUNSUPPORTED;
+    thc_sizes_t sz;
+    if ((rc = thc_sizes(ctx, list->d, 1, &sz)) != THC_OK) return rc;
+    VoidParams P;
+    memset(&P, 0, sizeof P);
+    P.norms = norms;
+    P.scales = scales;
+    P.out = out;
+    P.d = list->d;
+    P.scales_n = sz.scales_count;
+    P.n = list->n;
+    P.dev = view_of(ctx).dev;
+    struct Span { uint64_t lo, bytes; };
+    Span written[THC_MAX_WORKERS + 2], read[THC_MAX_WORKERS + 1];
+    uint32_t writes = 0, reads = 0;
+    written[writes++] = {reinterpret_cast<uint64_t>(out), list->d * 4u};
+    written[writes++] = {reinterpret_cast<uint64_t>(scales), P.scales_n * 4u};
+    read[reads++] = {reinterpret_cast<uint64_t>(norms), list->n * 4u};
+    if (ef_or_null != nullptr) {
+        P.residuals = list->n;
+        for (uint32_t i = 0; i < list->n; ++i) {
+            P.grads[i] = grads_or_null[i];
+            P.ef[i] = ef_or_null[i];
+            if (P.grads[i] == nullptr || !aligned16(P.grads[i]) || P.ef[i] == nullptr || !aligned16(P.ef[i])) return THC_EINVAL;
+            written[writes++] = {reinterpret_cast<uint64_t>(P.grads[i]), list->d * 4u};
+            read[reads++] = {reinterpret_cast<uint64_t>(P.ef[i]), list->d * 4u};
+        }
+    }
+    const auto apart = [](const Span &a, const Span &b) { return a.lo + a.bytes <= b.lo || b.lo + b.bytes <= a.lo; };
+    for (uint32_t i = 0; i < writes; ++i) {
+        for (uint32_t j = 0; j < i; ++j) if (!apart(written[i], written[j])) return THC_EINVAL;
+        for (uint32_t j = 0; j < reads; ++j) if (!apart(written[i], read[j])) return THC_EINVAL;
+    }
+    const uint64_t ctas = std::min<uint64_t>((list->d / 4u + kListThreads - 1) / kListThreads, 2ull * std::max(1u, list->sm_count));
+    THC_CUDA(launch_after(void_round_kernel, dim3((unsigned)ctas), kListThreads, 0, static_cast<cudaStream_t>(stream), P));
+    return THC_OK;
 }
 
 int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const thc_tensors *list, float *norms, void *workspace,

@@ -118,6 +118,10 @@ class CudaOps:
     def residual(self, grad, packed, rnd: int, scales, ef):
         self.ctx.error_feedback([grad], [packed], self.d, rnd, scales, [ef], self.workspace)
 
+    def void(self, tensors, norms, grad, scales, out, ef=None):
+        """After a round: nothing if `norms` (the sum of all ranks') is finite, else see thc.Context.void_round."""
+        self.ctx.void_round(tensors, norms, scales, out, None if ef is None else [grad], None if ef is None else [ef])
+
     def scatter(self, out, tensors, max_norm: float = math.inf):
         """The average, clipped by its norm, to tensors."""
         self.ctx.scatter_grads(out, max_norm, tensors, self.average_norm, self._workspace_of(tensors))
@@ -144,7 +148,7 @@ class DataParallelRound:
         self.ranges = block_ranges(self.nblocks, self.world)
         if (self.block * bits) % 128 != 0 and self.world > 1:
             raise ValueError("slices of packed indices must start on 16-byte boundaries")
-        self._recv = self._padded = self._gathered = self._total = None
+        self._recv = self._padded = self._gathered = self._total = self._norms = None
 
     def _idx_bytes(self, blocks: int) -> int:
         return blocks * self.block * self.bits // 8
@@ -205,9 +209,22 @@ class DataParallelRound:
 
     def step_tensors(self, tensors, rnd: int, max_norm: float = math.inf, ef=None):
         """step() with the rank's gradient tensors, clipped by their norm.  ef (fp32, the flat vector's length): the
-        residual of the rank's previous round, which is added, and replaced by this round's."""
+        residual of the rank's previous round, which is added, and replaced by this round's.
+
+        If any rank's norm is not finite the round is void on every rank: the average is NaN in every element and the residuals stay
+        as they were.  (In step() a rank's own scale of such a gradient is 0, but another rank's counts, and its indices, all
+        0, go into a finite average.)  The norms' sum over the ranks tells, one more all-reduce of four bytes; ops
+        without `norm`, what gather wrote, leave that out."""
         grad = self.ops.gather(tensors, max_norm, ef)
+        norm = getattr(self.ops, "norm", None)
+        if norm is not None:
+            if self._norms is None:
+                self._norms = torch.empty_like(norm)
+            self._norms.copy_(norm)
+            dist.all_reduce(self._norms, group=self.group)
         out, scales, packed, total = self.step(grad, rnd)
+        if norm is not None:
+            self.ops.void(tensors, self._norms, grad, scales, out, ef)
         if ef is not None:
             self.ops.residual(grad, packed, rnd, scales, ef)
         return out, scales, packed, total

@@ -103,7 +103,10 @@ class TensorRound:
     tensors (scatter) or through an Adam step into the weights (adamw).
 
     ``grads`` is a sequence of n sequences of tensors (see thc.Tensors).  With error feedback each worker's
-    residual of one round is added to its gradients of the next (fp32 contexts)."""
+    residual of one round is added to its gradients of the next (fp32 contexts).
+
+    A round in which a worker's norm is not finite is void: its average is NaN in every element, so that adamw takes no step and
+    scatter hands the NaN on, and every worker keeps its residual; the next round is as if it had not been."""
 
     def __init__(self, ctx: thc.Context, grads, error_feedback: bool = False):
         self.ctx = ctx
@@ -126,6 +129,7 @@ class TensorRound:
         r = self.round
         self.ctx.gather_grads(self.grads, max_norm, r.grads, self.norms, self.workspace, ef=self.ef, stream=stream)
         r.run(rnd, fused=True, stream=stream)
+        self.ctx.void_round(self.grads, self.norms, r.scales, r.out, None if self.ef is None else r.grads, self.ef, stream)
         if self.ef is not None:
             self.ctx.error_feedback(r.grads, r.packed, r.d, rnd, r.scales, self.ef, r.workspace, stream)
         return r.out

@@ -27,7 +27,8 @@ EXPORTS = ("thc_create", "thc_destroy", "thc_sizes", "thc_prepare", "thc_compres
            "thc_quantize_rotated", "thc_aggregate", "thc_decompress", "thc_aggregate_decompress", "thc_prepare_noalloc",
            "thc_error_feedback", "thc_accumulate_error", "thc_prepare_compress", "thc_prepare_minmax",
            "thc_tensors_create", "thc_tensors_destroy", "thc_tensors_sizes", "thc_tensors_offsets", "thc_tensors_assign",
-           "thc_grad_norm", "thc_clip_grads", "thc_gather_grads", "thc_scatter_grads", "thc_adamw", "thc_debug_skip_tasks", "thc_status", "thc_strerror", "thc_version")
+           "thc_grad_norm", "thc_clip_grads", "thc_gather_grads", "thc_void_round", "thc_scatter_grads", "thc_adamw",
+           "thc_debug_skip_tasks", "thc_status", "thc_strerror", "thc_version")
 NOALLOC_SCRATCH_BYTES = 4 << 20
 
 
@@ -110,6 +111,7 @@ def lib():
     L.thc_grad_norm.argtypes = [vp, vp, vp, vp, u64, vp]
     L.thc_clip_grads.argtypes = [vp, vp, f64, vp, vp, vp, u64, vp]
     L.thc_gather_grads.argtypes = [vp, vp, f64, pp, pp, vp, vp, u64, vp]
+    L.thc_void_round.argtypes = [vp, vp, vp, vp, vp, pp, pp, vp]
     L.thc_scatter_grads.argtypes = [vp, vp, f64, vp, vp, vp, u64, vp]
     L.thc_adamw.argtypes = [vp, ctypes.POINTER(_AdamwConfig), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     L.thc_debug_skip_tasks.argtypes = [vp, u32]
@@ -351,6 +353,11 @@ class Context:
         and norms = None: as they are."""
         _check(self._call.gather_grads(self._handle, tensors._handle, max_norm, ef, flats, norms, workspace,
                                        self.in_dtype == THC_BF16, stream), "thc_gather_grads")
+
+    def void_round(self, tensors: Tensors, norms, scales, out, grads=None, ef=None, stream=None):
+        """Behind the call that writes the average `out`, before `error_feedback`: if a worker's norm is not finite, the average
+        becomes NaN, the scales 0 and each of `grads` its residual `ef`, so that no residual changes and no step is taken."""
+        _check(self._call.void_round(self._handle, tensors._handle, norms, scales, out, grads, ef, stream), "thc_void_round")
 
     def scatter_grads(self, flat, max_norm: float, tensors: Tensors, norms, workspace, stream=None):
         """The flat average, clipped, to the tensors."""
