@@ -289,7 +289,7 @@ typedef struct thc_tensors thc_tensors;   /* opaque */
 typedef struct thc_tensors_sizes_t {
     uint64_t d;                /* length of the flat vector, a multiple of THC_TENSOR_ALIGN    */
     uint64_t elements;         /* elements of one worker's tensors                             */
-    uint64_t workspace_bytes;  /* scratch any of the calls may need for this list              */
+    uint64_t workspace_bytes;  /* scratch for any of the calls; the same for all lists of a device */
     uint32_t n;
     uint32_t count;
     int32_t device;            /* the context's, -1 without one                                */

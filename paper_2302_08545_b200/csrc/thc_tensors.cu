@@ -977,10 +977,13 @@ static NormShape norm_shape(const thc_tensors *h, uint32_t split_log2, bool alon
 
 static uint64_t round_up256(uint64_t v) { return (v + 255) / 256 * 256; }
 
-// Workspace: results of the workers, then the sums' partial results.
+// Workspace: results of the workers, then the sums' partial results.  The same for every list of a device, so that a program's one buffer
+// serves the gradients of n workers as well as the weights: norm_shape gives at most kNormMostRows rows of at most
+// max(1, kNormCtasPerSm sm_count / n) CTAs to each of n workers.
+static uint64_t results_bytes() { return round_up256(THC_MAX_WORKERS * sizeof(NormResult)); }
 static uint64_t workspace_need(const thc_tensors *h)
 {
-    return round_up256(h->n * sizeof(NormResult)) + round_up256((uint64_t)h->n * std::max(norm_shape(h, 0, false).ctas, norm_shape(h, 3, false).ctas) * sizeof(double));
+    return results_bytes() + round_up256((uint64_t)kNormMostRows * std::max(h->sm_count * kNormCtasPerSm, THC_MAX_WORKERS) * sizeof(double));
 }
 
 int thc_tensors_sizes(const thc_tensors *h, thc_tensors_sizes_t *s)
@@ -1078,7 +1081,7 @@ static void fill_params(ListParams &P, const thc_ctx *ctx, const thc_tensors *h,
     P.max_norm = max_norm;
     P.norms = norms;
     P.result = static_cast<NormResult *>(workspace);
-    P.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + round_up256(h->n * sizeof(NormResult)));
+    P.partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + results_bytes());
     P.dev = view_of(ctx).dev;
 }
 

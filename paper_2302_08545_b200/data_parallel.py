@@ -102,7 +102,7 @@ class CudaOps:
     def _workspace_of(self, tensors):
         if tensors.d != self.d or tensors.n != 1:
             raise ValueError(f"a list of one worker whose flat vector has {self.d} elements is expected")
-        if self._list_workspace is None or self._list_workspace.nbytes < tensors.workspace_bytes:
+        if self._list_workspace is None:                             # serves every list
             self._list_workspace = torch.empty(tensors.workspace_bytes, dtype=torch.uint8, device=self.device)
         return self._list_workspace
 

@@ -115,14 +115,8 @@ class TensorRound:
         self.round = Round(ctx, n, d, "bf16" if ctx.in_dtype == thc.THC_BF16 else "f32", device=device)
         self.norms = torch.zeros(n, dtype=torch.float32, device=device)
         self.average_norm = torch.zeros(1, dtype=torch.float32, device=device)
-        self.workspace = None
-        self._workspace_of(self.grads)
+        self.workspace = torch.empty(self.grads.workspace_bytes, dtype=torch.uint8, device=device)    # serves every list
         self.ef = [torch.zeros(d, dtype=torch.float32, device=device) for _ in range(n)] if error_feedback else None
-
-    def _workspace_of(self, tensors: thc.Tensors):
-        if self.workspace is None or self.workspace.nbytes < tensors.workspace_bytes:
-            self.workspace = torch.empty(tensors.workspace_bytes, dtype=torch.uint8, device=self.round.device)
-        return self.workspace
 
     def run(self, rnd: int = 0, max_norm: float = math.inf, stream=None):
         """Gather and the round; returns the flat average (a buffer of this object)."""
@@ -136,9 +130,9 @@ class TensorRound:
 
     def scatter(self, tensors: thc.Tensors, max_norm: float = math.inf, stream=None):
         """The average, clipped by its norm, to the tensors of a list with one worker."""
-        self.ctx.scatter_grads(self.round.out, max_norm, tensors, self.average_norm, self._workspace_of(tensors), stream)
+        self.ctx.scatter_grads(self.round.out, max_norm, tensors, self.average_norm, self.workspace, stream)
 
     def adamw(self, weights: thc.Tensors, lr, step, m, v, master=None, stream=None, **how):
         """An Adam step with the average (arguments as thc.Context.adamw)."""
-        self.ctx.adamw(self.round.out, weights, lr, step, m, v, self.average_norm, self._workspace_of(weights),
+        self.ctx.adamw(self.round.out, weights, lr, step, m, v, self.average_norm, self.workspace,
                        master=master, stream=stream, **how)

@@ -175,7 +175,7 @@ class Tensors:
 
     ``workers`` is a sequence of n sequences of tensors.  In a flat vector of ``d`` elements tensor t
     starts at ``offsets[t]``; ``views(flat)`` are the tensors' places in it.  ``workspace_bytes`` is what
-    the calls that take the list need.  A tensor that is later given other memory (``set_``, a new
+    the calls that take a list need, the same for all lists of a device.  A tensor that is later given other memory (``set_``, a new
     ``.grad``) is not followed: ``assign`` takes the new ones.  A CUDA graph that holds calls on a list needs
     the list as long as it is replayed.  Calls write behind autograd's back."""
 
