@@ -70,7 +70,7 @@ class CudaOps:
         self.norm = torch.zeros(1, dtype=torch.float32, device=device)       # of the rank's own gradients
         self.average_norm = torch.zeros(1, dtype=torch.float32, device=device)
         self._part = {}
-        self._flat = self._list_workspace = None
+        self._flat = self._list_workspace = self._offsets = None
 
     def local_scales(self, grad):
         self.ctx.prepare([grad], self.d, self.scales, self.workspace)
@@ -98,12 +98,16 @@ class CudaOps:
         self.ctx.decompress(total, divisor, self.d, rnd, scales, self.out, self.workspace)
         return self.out
 
-    # -- between the round and a program's tensors (thc.Tensors with one worker and d = the round's)
+    # -- between the round and a program's tensors (thc.Tensors with one worker and d = the round's; all with the places of the
+    # first one's tensors in the flat vector)
     def _workspace_of(self, tensors):
         if tensors.d != self.d or tensors.n != 1:
             raise ValueError(f"a list of one worker whose flat vector has {self.d} elements is expected")
         if self._list_workspace is None:                             # serves every list
             self._list_workspace = torch.empty(tensors.workspace_bytes, dtype=torch.uint8, device=self.device)
+            self._offsets = tensors.offsets
+        if tensors.offsets != self._offsets:
+            raise ValueError("a list whose tensors have the places of the first list's in the flat vector is expected")
         return self._list_workspace
 
     def gather(self, tensors, max_norm: float = math.inf, ef=None):

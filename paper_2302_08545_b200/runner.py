@@ -118,6 +118,10 @@ class TensorRound:
         self.workspace = torch.empty(self.grads.workspace_bytes, dtype=torch.uint8, device=device)    # serves every list
         self.ef = [torch.zeros(d, dtype=torch.float32, device=device) for _ in range(n)] if error_feedback else None
 
+    def _check(self, tensors: thc.Tensors):
+        if tensors.n != 1 or not tensors.same_layout(self.grads):
+            raise ValueError("a list of one worker with the places of the gradients in the flat vector is expected")
+
     def run(self, rnd: int = 0, max_norm: float = math.inf, stream=None):
         """Gather and the round; returns the flat average (a buffer of this object)."""
         r = self.round
@@ -129,10 +133,12 @@ class TensorRound:
         return r.out
 
     def scatter(self, tensors: thc.Tensors, max_norm: float = math.inf, stream=None):
-        """The average, clipped by its norm, to the tensors of a list with one worker."""
+        """The average, clipped by its norm, to the tensors of a list with one worker and the gradients' sizes."""
+        self._check(tensors)
         self.ctx.scatter_grads(self.round.out, max_norm, tensors, self.average_norm, self.workspace, stream)
 
     def adamw(self, weights: thc.Tensors, lr, step, m, v, master=None, stream=None, **how):
         """An Adam step with the average (arguments as thc.Context.adamw)."""
+        self._check(weights)
         self.ctx.adamw(self.round.out, weights, lr, step, m, v, self.average_norm, self.workspace,
                        master=master, stream=stream, **how)

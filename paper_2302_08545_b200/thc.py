@@ -240,6 +240,10 @@ class Tensors:
         _check(lib().thc_tensors_assign(self._ctx._h, self._h, addresses, _stream(stream)), "thc_tensors_assign")
         self.tensors = workers
 
+    def same_layout(self, other: "Tensors") -> bool:
+        """Whether both lists' tensors have the same places in a flat vector."""
+        return self.d == other.d and self.offsets == other.offsets
+
     def views(self, flat):
         return [flat[o: o + math.prod(s)].view(s) for o, s in zip(self.offsets, self.shapes)]
 
