@@ -335,6 +335,42 @@ static int list_stream(PyObject *o, const thc_tensors_sizes_t *sz, void **st)
     return stream_of(o, st);
 }
 
+/* What a tensor is, if it is contiguous and on the list's device (1; else 0, or -1 with an exception set).  `type` is NULL where torch's
+ * table describes it, which then tells in `kind`. */
+typedef struct { void *p; uint64_t bytes; PyObject *type; dl_type kind; } block_t;
+static int block_of(PyObject *o, const thc_tensors_sizes_t *sz, block_t *b)
+{
+    dl_tensor d;
+    memset(&d, 0, sizeof d);
+    memset(b, 0, sizeof *b);
+    if (exchange != NULL && exchange->describe(o, &d) == 0) {
+        uint64_t n = 1;
+        int ok = 1;
+        for (int32_t i = d.ndim; i-- > 0;) {
+            if (d.strides != NULL && d.shape[i] > 1 && d.strides[i] != (int64_t)n) ok = 0;
+            n *= (uint64_t)d.shape[i];
+        }
+        const int cuda = d.device.type == DL_CUDA;
+        b->p = (char *)d.data + d.byte_offset;
+        b->bytes = n * d.dtype.bits / 8u * d.dtype.lanes;
+        b->kind = d.dtype;
+        return ok && (cuda || d.device.type == DL_CPU) && (cuda ? d.device.id : -1) == sz->device;
+    }
+    PyErr_Clear();
+    if (address(o, &b->p) != 0) return -1;
+    PyObject *t = PyObject_GetAttr(o, s_dtype), *c = PyObject_CallMethodNoArgs(o, s_is_contiguous), *v = PyObject_GetAttr(o, s_nbytes),
+             *g = PyObject_CallMethodNoArgs(o, s_get_device);
+    int ok = t != NULL && c != NULL && v != NULL && g != NULL && number(v, &b->bytes) == 0;
+    const long device = ok ? PyLong_AsLong(g) : 0;
+    ok = ok && c == Py_True && device == sz->device;
+    b->type = t;                                          /* (torch's types are never freed) */
+    Py_XDECREF(t);
+    Py_XDECREF(c);
+    Py_XDECREF(v);
+    Py_XDECREF(g);
+    return PyErr_Occurred() ? -1 : ok;
+}
+
 enum { F32, BF16, I64 };
 static int vector(PyObject *o, void **p, int type, uint64_t elements, const thc_tensors_sizes_t *sz, const char *what)
 {
@@ -342,39 +378,33 @@ static int vector(PyObject *o, void **p, int type, uint64_t elements, const thc_
     const int is = PyObject_IsInstance(o, tensor_type);
     if (is < 0) return -1;
     if (is == 0) return address(o, p);
-    int ok;
-    dl_tensor d;
-    memset(&d, 0, sizeof d);
-    if (exchange != NULL && exchange->describe(o, &d) == 0) {
-        uint64_t n = 1;
-        ok = 1;
-        for (int32_t i = d.ndim; i-- > 0;) {
-            if (d.strides != NULL && d.shape[i] > 1 && d.strides[i] != (int64_t)n) ok = 0;
-            n *= (uint64_t)d.shape[i];
-        }
-        const int cuda = d.device.type == DL_CUDA;
-        ok = ok && n >= elements && d.dtype.lanes == 1 && (cuda || d.device.type == DL_CPU) && (cuda ? d.device.id : -1) == sz->device &&
-             d.dtype.code == (type == F32 ? DL_FLOAT : type == BF16 ? DL_BFLOAT : DL_INT) && d.dtype.bits == (type == F32 ? 32 : type == BF16 ? 16 : 64);
-        *p = (char *)d.data + d.byte_offset;
-    } else {
-        PyErr_Clear();
-        if (address(o, p) != 0) return -1;
-        PyObject *t = PyObject_GetAttr(o, s_dtype), *c = PyObject_CallMethodNoArgs(o, s_is_contiguous), *v = PyObject_GetAttr(o, s_nbytes),
-                 *g = PyObject_CallMethodNoArgs(o, s_get_device);
-        uint64_t bytes = 0;
-        ok = t != NULL && c != NULL && v != NULL && g != NULL && number(v, &bytes) == 0;
-        const long device = ok ? PyLong_AsLong(g) : 0;
-        ok = ok && t == (type == F32 ? t_f32 : type == BF16 ? t_bf16 : t_i64) && c == Py_True && device == sz->device &&
-             bytes >= elements * (type == F32 ? 4u : type == BF16 ? 2u : 8u);
-        Py_XDECREF(t);
-        Py_XDECREF(c);
-        Py_XDECREF(v);
-        Py_XDECREF(g);
-        if (PyErr_Occurred()) return -1;
-    }
-    if (ok) return 0;
+    block_t b;
+    int ok = block_of(o, sz, &b);
+    if (ok < 0) return -1;
+    const uint32_t size = type == F32 ? 4u : type == BF16 ? 2u : 8u;
+    if (b.type != NULL) ok = ok && b.type == (type == F32 ? t_f32 : type == BF16 ? t_bf16 : t_i64);
+    else ok = ok && b.kind.lanes == 1 && b.kind.bits == size * 8u && b.kind.code == (type == F32 ? DL_FLOAT : type == BF16 ? DL_BFLOAT : DL_INT);
+    *p = b.p;
+    if (ok && b.bytes >= elements * size) return 0;
     PyErr_Format(PyExc_ValueError, "%s: a contiguous %s tensor of at least %llu elements on the context's device is expected", what,
                  type == F32 ? "float32" : type == BF16 ? "bfloat16" : "int64", (unsigned long long)elements);
+    return -1;
+}
+
+/* Workspace of a call on a list: a tensor of any type, contiguous and on the list's device; anything else as for the other calls. */
+static int list_workspace(PyObject *o, void **p, uint64_t *bytes, const thc_tensors_sizes_t *sz)
+{
+    if (o == Py_None || sz->n == 0) return workspace(o, p, bytes);
+    const int is = PyObject_IsInstance(o, tensor_type);
+    if (is < 0) return -1;
+    if (is == 0) return workspace(o, p, bytes);
+    block_t b;
+    const int ok = block_of(o, sz, &b);
+    if (ok < 0) return -1;
+    *p = b.p;
+    *bytes = b.bytes;
+    if (ok && b.p != NULL) return 0;
+    PyErr_SetString(PyExc_ValueError, "workspace: a contiguous tensor on the context's device is expected");
     return -1;
 }
 
@@ -421,7 +451,7 @@ static PyObject *b_grad_norm(ARGS)
 {
     LIST_CALL(5, 1);
     void *norms;
-    if (vector(a[2], &norms, F32, sz.n, &sz, "norms") || workspace(a[3], &ws, &wb)) return NULL;
+    if (vector(a[2], &norms, F32, sz.n, &sz, "norms") || list_workspace(a[3], &ws, &wb, &sz)) return NULL;
     CALL(thc_grad_norm(ctx, list, norms, ws, wb, st));
 }
 
@@ -432,7 +462,7 @@ static PyObject *b_clip_grads(ARGS)
     double most;
     void *out, *norms;
     if (real(a[2], &most) || address(a[3], &out) || vector(a[4], &norms, F32, sz.n, &sz, "norms") ||
-        workspace(a[5], &ws, &wb)) return NULL;
+        list_workspace(a[5], &ws, &wb, &sz)) return NULL;
     CALL(thc_clip_grads(ctx, list, most, out, norms, ws, wb, st));
 }
 
@@ -445,7 +475,7 @@ static PyObject *b_gather_grads(ARGS)
     void *norms;
     const int type = PyObject_IsTrue(a[7]) ? BF16 : F32;
     if (real(a[2], &most) || vectors(a[3], &e, F32, &sz, "ef") || vectors(a[4], &f, type, &sz, "flats") ||
-        vector(a[5], &norms, F32, sz.n, &sz, "norms") || workspace(a[6], &ws, &wb)) return NULL;
+        vector(a[5], &norms, F32, sz.n, &sz, "norms") || list_workspace(a[6], &ws, &wb, &sz)) return NULL;
     CALL(thc_gather_grads(ctx, list, most, (const float *const *)array_of(&e), array_of(&f), norms, ws, wb, st));
 }
 
@@ -474,7 +504,7 @@ static PyObject *b_scatter_grads(ARGS)
     double most;
     void *flat, *norms;
     if (vector(a[1], &flat, F32, sz.d, &sz, "flat") || real(a[2], &most) ||
-        vector(a[4], &norms, F32, sz.n, &sz, "norms") || workspace(a[5], &ws, &wb)) return NULL;
+        vector(a[4], &norms, F32, sz.n, &sz, "norms") || list_workspace(a[5], &ws, &wb, &sz)) return NULL;
     CALL(thc_scatter_grads(ctx, flat, most, list, norms, ws, wb, st));
 }
 
@@ -488,7 +518,7 @@ static PyObject *b_adamw(ARGS)
     if (vector(a[2], &grad, F32, sz.d, &sz, "grad") || vector(a[4], &lr, F32, 1, &sz, "lr") ||
         vector(a[5], &step, I64, 1, &sz, "step") || vector(a[6], &master, F32, sz.d, &sz, "master") ||
         vector(a[7], &m, F32, sz.d, &sz, "m") || vector(a[8], &v, F32, sz.d, &sz, "v") ||
-        vector(a[9], &decay, F32, sz.count, &sz, "decay") || vector(a[10], &norms, F32, 1, &sz, "norms") || workspace(a[11], &ws, &wb)) return NULL;
+        vector(a[9], &decay, F32, sz.count, &sz, "decay") || vector(a[10], &norms, F32, 1, &sz, "norms") || list_workspace(a[11], &ws, &wb, &sz)) return NULL;
     CALL(thc_adamw(ctx, &cfg, grad, list, lr, step, master, m, v, decay, norms, ws, wb, st));
 }
 
