@@ -314,7 +314,8 @@ int thc_tensors_offsets(const thc_tensors *list, uint64_t *offsets);
 
 /* New addresses for the same sizes and types (gradients that are allocated anew every step), from the calls
  * on that are issued on `stream` afterwards.  Allocates nothing; may be captured (a replay sets the addresses
- * that were given at capture, which the checks of later calls do not know of). */
+ * that were given at capture, which the checks of later calls do not know of).  Where it fails the list is as before; if
+ * only some of its launches went out (THC_ECUDA, lists of more than 448 addresses), calls on it are THC_EINVAL until an assignment succeeds. */
 int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *list, const void *const *tensors, void *stream);
 
 /* Global L2 norm of each worker's tensors: norms[i] = sqrt(sum over all tensors of worker i of x^2).  Squares of

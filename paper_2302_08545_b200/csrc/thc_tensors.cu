@@ -820,6 +820,7 @@ struct thc_tensors {
     struct Range { uint64_t lo, hi; uint32_t index; };
     std::vector<Range> ranges;                 // of the tensors that are not empty, by address
     bool overlapping;                          // tensors of the list overlap each other
+    bool torn;                                 // an assignment failed when part of the device's table had been set
     uint64_t *base;                            // the allocation; pieces are in it
     Piece *pieces;
 };
@@ -895,6 +896,7 @@ int thc_tensors_create(const thc_ctx *ctx, const void *const *tensors, const uin
         h->d = d;
         h->elements = elements;
         h->all_f32 = true;
+        h->torn = false;
         h->pieces = nullptr;
         h->base = nullptr;
         h->numel.assign(numel, numel + count);
@@ -1007,7 +1009,7 @@ int thc_tensors_offsets(const thc_tensors *h, uint64_t *offsets)
 }
 
 // A list can be used where its context can launch.
-static int check_list(const thc_ctx *ctx, const thc_tensors *h)
+static int check_list_device(const thc_ctx *ctx, const thc_tensors *h)
 {
     if (ctx == nullptr || h == nullptr) return THC_EINVAL;
     const int rc = check_launch_ctx(ctx);
@@ -1015,9 +1017,15 @@ static int check_list(const thc_ctx *ctx, const thc_tensors *h)
     return h->device == view_of(ctx).device ? THC_OK : THC_EINVAL;
 }
 
+static int check_list(const thc_ctx *ctx, const thc_tensors *h)
+{
+    const int rc = check_list_device(ctx, h);
+    return rc == THC_OK && h->torn ? THC_EINVAL : rc;
+}
+
 int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *h, const void *const *tensors, void *stream)
 {
-    int rc = check_list(ctx, h);
+    int rc = check_list_device(ctx, h);
     if (rc != THC_OK) return rc;
     if (tensors == nullptr) return THC_EINVAL;
     try {
@@ -1025,19 +1033,22 @@ int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *h, const void *const *te
         std::vector<thc_tensors::Range> old_ranges = h->ranges;
         const bool old_overlapping = h->overlapping;
         rc = take_addresses(h, tensors);
-        for (size_t i = 0; rc == THC_OK && i < h->address.size(); i += kAssignMost) {
+        size_t set = 0;
+        while (rc == THC_OK && set < h->address.size()) {
             AssignParams P;
-            P.to = h->base + i;
-            P.n = (uint32_t)std::min<size_t>(kAssignMost, h->address.size() - i);
-            for (uint32_t j = 0; j < P.n; ++j) P.base[j] = base_of(h, i + j);
+            P.to = h->base + set;
+            P.n = (uint32_t)std::min<size_t>(kAssignMost, h->address.size() - set);
+            for (uint32_t j = 0; j < P.n; ++j) P.base[j] = base_of(h, set + j);
             const cudaError_t e = launch_after(list_assign_kernel, dim3(1), (kAssignMost + 31) / 32 * 32, 0, static_cast<cudaStream_t>(stream), P);
-            if (e != cudaSuccess) return cuda_fail(e);
+            if (e != cudaSuccess) rc = cuda_fail(e);
+            else set += P.n;
         }
-        if (rc != THC_OK) {
+        if (rc != THC_OK) {                    // the checks of later calls go by what the device's table holds
             h->address.swap(old_address);
             h->ranges.swap(old_ranges);
             h->overlapping = old_overlapping;
         }
+        if (rc == THC_OK || set != 0) h->torn = rc != THC_OK;
     } catch (const std::bad_alloc &) {
         return THC_EINVAL;
     }
