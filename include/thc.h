@@ -321,7 +321,9 @@ int thc_tensors_assign(const thc_ctx *ctx, thc_tensors *list, const void *const 
 /* Global L2 norm of each worker's tensors: norms[i] = sqrt(sum over all tensors of worker i of x^2).  Squares of
  * fp32 are summed in fp64, those of 16-bit types eight at a time in fp32 (which moves the norm by at most
  * 1.5 x 2^-24 of it) and then in fp64, in a fixed order (the same bits on every call).  A tensor that stands in the list
- * twice counts twice.  A norm that is NaN or infinite sets THC_STATUS_NONFINITE.
+ * twice counts twice.  A norm that is NaN or infinite sets THC_STATUS_NONFINITE.  Here and in the calls below that is the norm in fp64, as is
+ * what they clip by: one of finite values past fp32's end is stored as infinity, without the status bit, and is clipped by
+ * (and thc_adamw takes the step) like any other.
  *   norms  device, n fp32, written (4-byte aligned, here and below)                              */
 int thc_grad_norm(thc_ctx *ctx, const thc_tensors *list, float *norms, void *workspace, uint64_t workspace_bytes,
                   void *stream);
@@ -370,7 +372,7 @@ int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const th
 /* The Adam step with decoupled weight decay on the flat average (g = c x, clipped as above):
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,   t = step + 1,
  *     w = w (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
- * If the norm is not finite nothing is updated, step included, and THC_STATUS_NONFINITE is set.  Learning
+ * If the norm is not finite (in fp64, see thc_grad_norm) nothing is updated, step included, and THC_STATUS_NONFINITE is set.  Learning
  * rate and step count are read on the device, so that a captured step can be replayed.
  *   grad    device, sizes.d fp32, read
  *   list    n = 1: the model's weights, written

@@ -342,7 +342,8 @@ class Context:
 
     # -- lists of tensors; norms: float32, one per worker
     def grad_norm(self, tensors: Tensors, norms, workspace, stream=None):
-        """The global L2 norm of each worker's tensors."""
+        """The global L2 norm of each worker's tensors (infinity where it is past fp32's end; only of values that are not finite with a
+        status bit)."""
         _check(self._call.grad_norm(self._handle, tensors._handle, norms, workspace, stream), "thc_grad_norm")
 
     def clip_grads(self, tensors: Tensors, max_norm: float, norms, workspace, out: Tensors | None = None, stream=None):
