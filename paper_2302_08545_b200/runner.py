@@ -102,7 +102,8 @@ class TensorRound:
     worker's norm, become the flat vectors that the round compresses; its average goes, clipped again, back to
     tensors (scatter) or through an Adam step into the weights (adamw).
 
-    ``grads`` is a sequence of n sequences of tensors (see thc.Tensors).  With error feedback each worker's
+    ``grads`` is a sequence of n sequences of tensors (see thc.Tensors), which the object keeps and reads every round: gradients
+    that are allocated anew every step (torch's zero_grad sets them to None) are given to it by assign.  With error feedback each worker's
     residual of one round is added to its gradients of the next (fp32 contexts).
 
     A round in which a worker's norm is not finite is void: its average is NaN in every element, so that adamw takes no step and
@@ -117,6 +118,10 @@ class TensorRound:
         self.average_norm = torch.zeros(1, dtype=torch.float32, device=device)
         self.workspace = torch.empty(self.grads.workspace_bytes, dtype=torch.uint8, device=device)    # serves every list
         self.ef = [torch.zeros(d, dtype=torch.float32, device=device) for _ in range(n)] if error_feedback else None
+
+    def assign(self, grads, stream=None):
+        """Other gradient tensors of the same shapes and types, for the rounds issued on ``stream`` from here on."""
+        self.grads.assign(grads, stream)
 
     def _check(self, tensors: thc.Tensors):
         if tensors.n != 1 or not tensors.same_layout(self.grads):
