@@ -137,7 +137,8 @@ template <uint32_t T>
 __device__ __forceinline__ uint32_t head_of(uint64_t a) { return (uint32_t)((0ull - a) / size_of<T>()) & (kUnit - 1u); }
 
 // ---------------------------------------------------------------------------------- held units
-// Units of the pieces that a warp read last, in its part of shared memory; a lane reads what it wrote itself.
+// Units of the item that a warp of the cluster has read, in its part of shared memory (at address `held`); a lane reads what it wrote
+// itself.
 // 16 bytes of a lane next to its neighbours': no bank conflicts.
 template <uint32_t T>
 __device__ __forceinline__ void hold_unit(uint32_t held, uint32_t b, uint32_t lane, const Raw<T> &r)
@@ -160,7 +161,6 @@ __device__ __forceinline__ Raw<T> held_unit(uint32_t held, uint32_t b, uint32_t 
                      : "r"(held + (b * kParts + i) * 512u + lane * 16u));
     return r;
 }
-constexpr uint32_t kNotHeld = 0xFFFFFFFFu;
 
 // ---------------------------------------------------------------------------------- norm
 // s + the squares of a unit.  fp32: each square in fp64, which no value leaves.  16 bits: the squares are exact in fp32, eight
@@ -197,7 +197,7 @@ __device__ __forceinline__ void add_squares(double (&s)[2], const Raw<T> &r)
     }
 }
 
-// Sum of squares of a piece, in a lane; its units go to `held` unless that is kNotHeld.
+// Sum of squares of a piece, in a lane; HOLD: its units go to `held`.
 template <uint32_t T, bool HOLD>
 __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uint32_t lane, uint32_t held)
 {
@@ -219,7 +219,7 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
             r[b] = load_unit8<T>(at + (kWhole ? lane + 32u * b : min(lane + 32u * b, left - 1u)) * (kUnit * size_of<T>()));
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-            if (HOLD && held != kNotHeld) hold_unit<T>(held, first + b, lane, r[b]);
+            if (HOLD) hold_unit<T>(held, first + b, lane, r[b]);
             if (!kWhole && lane + 32u * b >= left) r[b] = Raw<T>{};
             add_squares<T>(s, r[b]);
         }
@@ -235,7 +235,7 @@ __device__ __forceinline__ double squares_of_piece(uint64_t a, uint32_t len, uin
 }
 
 template <bool HOLD>
-__device__ __forceinline__ double squares(const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane, uint32_t held)
+__device__ __forceinline__ double squares(const Piece &p, const uint64_t *base, uint64_t flat, uint32_t lane, uint32_t held = 0)
 {
     const uint32_t len = p.len_type & 0xFFFFu, type = p.len_type >> 16;
     if (flat != 0) return squares_of_piece<THC_F32, HOLD>(flat + p.flat * 4u, len, lane, held);
@@ -259,8 +259,8 @@ __device__ __forceinline__ double sum_of_cta(double s, double (&red)[WARPS])
 }
 
 // ---------------------------------------------------------------------------------- products
-// y = c x (+ e) for a piece, whose units are in `held` unless that is kNotHeld; zeros (or e) from its end up to dst_len.
-template <uint32_t S, uint32_t D, bool EF>
+// y = c x (+ e) for a piece, whose units are in `held` (HELD) or in memory; zeros (or e) from its end up to dst_len.
+template <uint32_t S, uint32_t D, bool EF, bool HELD>
 __device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t ef, uint32_t len, uint32_t dst_len, const Factor &c, uint32_t lane, uint32_t held)
 {
     const auto product = [&c](float x, float e) { return EF ? fmaf(c.factor, x * c.scale, e) : times(c, x); };
@@ -278,7 +278,7 @@ __device__ __forceinline__ void move_piece(uint64_t src, uint64_t dst, uint64_t 
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 const uint32_t v = (kWhole ? lane + 32u * b : min(lane + 32u * b, left - 1u)) * kUnit;
-                x[b] = held != kNotHeld ? held_unit<S>(held, first + b, lane) : load_unit8<S>(s + v * size_of<S>());
+                x[b] = HELD ? held_unit<S>(held, first + b, lane) : load_unit8<S>(s + v * size_of<S>());
                 if constexpr (EF) r[b] = load_unit8<THC_F32>(q + v * 4u);
             }
             first += kBatch;
@@ -374,7 +374,7 @@ __device__ __forceinline__ AdamPlace adam_place(const AdamParams &P, const Piece
 }
 
 struct AdamUnit { Raw<THC_F32> g, m, v, w; };
-template <bool MASTER>
+template <bool MASTER, bool HELD>
 __device__ __forceinline__ AdamUnit adam_load(const AdamPlace &a, uint32_t u, uint32_t held, uint32_t lane)
 {
     const uint64_t o = (uint64_t)u * (kUnit * 4u);
@@ -385,12 +385,12 @@ __device__ __forceinline__ AdamUnit adam_load(const AdamPlace &a, uint32_t u, ui
     else
 #pragma unroll
         for (int e = 0; e < 8; ++e) r.w.w[e] = ld_global(reinterpret_cast<const uint32_t *>(a.w + o + 4u * e));
-    r.g = held != kNotHeld ? held_unit<THC_F32>(held, u / 32u, lane) : load_unit8<THC_F32>(a.g + o);
+    r.g = HELD ? held_unit<THC_F32>(held, u / 32u, lane) : load_unit8<THC_F32>(a.g + o);
     return r;
 }
 
 // The step of an item; `cur` is the lane's first unit, if it has one.
-template <uint32_t T, bool MASTER>
+template <uint32_t T, bool MASTER, bool HELD>
 __device__ __forceinline__ void adam_item(const AdamPlace &a, const AdamStep &k, AdamUnit cur, uint32_t lane, uint32_t held)
 {
     const bool whole = head_of<T>(a.out) == 0u;
@@ -398,7 +398,7 @@ __device__ __forceinline__ void adam_item(const AdamPlace &a, const AdamStep &k,
     for (uint32_t u = lane; u < a.units; u += 32u) {
         const uint64_t o = (uint64_t)u * (kUnit * 4u), to = a.out + (uint64_t)u * (kUnit * size_of<T>());
         AdamUnit next{};
-        if (u + 32u < a.units) next = adam_load<MASTER>(a, u + 32u, held, lane);
+        if (u + 32u < a.units) next = adam_load<MASTER, HELD>(a, u + 32u, held, lane);
         float ym[8], yv[8], yw[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -471,21 +471,21 @@ __device__ __forceinline__ ItemBase load_item_base(const ListParams &P, const Pi
     return ItemBase{load_base(P.L.base + i), K == kClip ? load_base(P.dst_base + i) : 0};
 }
 
-template <ClipKind K, uint32_t T>
+template <ClipKind K, uint32_t T, bool HELD>
 __device__ __forceinline__ void move_typed(const ParamsOf<K> &P, const Piece &p, const ItemBase &base, uint32_t worker, const Factor &c, uint32_t lane,
                                            uint32_t held)
 {
     const uint32_t len = p.len_type & 0xFFFFu;
     const uint64_t at = p.flat * size_of<T>(), tensor = base.tensor + at;
     if constexpr (K == kClip) {
-        move_piece<T, T, false>(tensor, base.dst + at, 0, len, len, c, lane, held);
+        move_piece<T, T, false, HELD>(tensor, base.dst + at, 0, len, len, c, lane, held);
     } else if constexpr (K == kScatter) {
-        move_piece<THC_F32, T, false>(P.src_flat + p.flat * 4u, tensor, 0, len, len, c, lane, held);
+        move_piece<THC_F32, T, false, HELD>(P.src_flat + p.flat * 4u, tensor, 0, len, len, c, lane, held);
     } else {
         constexpr uint32_t D = K == kGatherBf16 ? THC_BF16 : THC_F32;
         const uint32_t full = (len + THC_TENSOR_ALIGN - 1u) / THC_TENSOR_ALIGN * THC_TENSOR_ALIGN;
-        move_piece<T, D, K == kGatherResidual>(tensor, P.dst_flat[worker] + p.flat * size_of<D>(),
-                                               K == kGatherResidual ? P.ef[worker] + p.flat * 4u : 0, len, full, c, lane, held);
+        move_piece<T, D, K == kGatherResidual, HELD>(tensor, P.dst_flat[worker] + p.flat * size_of<D>(),
+                                                     K == kGatherResidual ? P.ef[worker] + p.flat * 4u : 0, len, full, c, lane, held);
     }
 }
 
@@ -497,33 +497,33 @@ struct Early<kAdam> { AdamPlace place; AdamUnit first; float decay; };
 template <>
 struct Early<kAdamMaster> : Early<kAdam> {};
 
-template <ClipKind K>
-__device__ __forceinline__ Early<K> load_early(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t lane, uint32_t held)
+template <ClipKind K, bool HELD>
+__device__ __forceinline__ Early<K> load_early(const ListParams &P, const Piece &p, const ItemBase &base, uint32_t lane, uint32_t held = 0)
 {
     Early<K> r{};
     if constexpr (is_adam(K)) {
         r.place = adam_place<K == kAdamMaster>(P.adam, p, base.tensor);
-        if (lane < r.place.units) r.first = adam_load<K == kAdamMaster>(r.place, lane, held, lane);
+        if (lane < r.place.units) r.first = adam_load<K == kAdamMaster, HELD>(r.place, lane, held, lane);
         if (P.adam.decay != nullptr) r.decay = ld_global(P.adam.decay + p.tensor);
     }
     return r;
 }
 
-template <ClipKind K>
+template <ClipKind K, bool HELD>
 __device__ __forceinline__ void products(const ParamsOf<K> &P, const Piece &p, const ItemBase &base, const Early<K> &early, uint32_t worker, AdamStep &k,
-                                         float lr, uint32_t lane, uint32_t held)
+                                         float lr, uint32_t lane, uint32_t held = 0)
 {
     const uint32_t type = p.len_type >> 16;
     if constexpr (is_adam(K)) {
         constexpr bool kMaster = K == kAdamMaster;
         k.keep = (float)(1.0 - (double)lr * (P.adam.decay != nullptr ? (double)early.decay : P.adam.weight_decay));
-        if (!kMaster || type == THC_F32) adam_item<THC_F32, kMaster>(early.place, k, early.first, lane, held);
-        else if (type == THC_BF16) adam_item<THC_BF16, kMaster>(early.place, k, early.first, lane, held);
-        else adam_item<THC_F16, kMaster>(early.place, k, early.first, lane, held);
+        if (!kMaster || type == THC_F32) adam_item<THC_F32, kMaster, HELD>(early.place, k, early.first, lane, held);
+        else if (type == THC_BF16) adam_item<THC_BF16, kMaster, HELD>(early.place, k, early.first, lane, held);
+        else adam_item<THC_F16, kMaster, HELD>(early.place, k, early.first, lane, held);
     } else {
-        if (type == THC_F32) move_typed<K, THC_F32>(P, p, base, worker, k.c, lane, held);
-        else if (type == THC_BF16) move_typed<K, THC_BF16>(P, p, base, worker, k.c, lane, held);
-        else move_typed<K, THC_F16>(P, p, base, worker, k.c, lane, held);
+        if (type == THC_F32) move_typed<K, THC_F32, HELD>(P, p, base, worker, k.c, lane, held);
+        else if (type == THC_BF16) move_typed<K, THC_BF16, HELD>(P, p, base, worker, k.c, lane, held);
+        else move_typed<K, THC_F16, HELD>(P, p, base, worker, k.c, lane, held);
     }
 }
 
@@ -573,7 +573,7 @@ list_norm_kernel(const __grid_constant__ ListParams P)
         const Piece now = p;
         c += stride;
         if (c < end) p = load_item(P.L, c, P.split_log2);
-        s += squares<false>(now, base, P.src_flat, lane, kNotHeld);
+        s += squares<false>(now, base, P.src_flat, lane);
     }
     __shared__ double red[kListWarps];
     __shared__ NormResult s_result;
@@ -638,7 +638,7 @@ list_product_kernel(const __grid_constant__ ParamsOf<K> P)
             sum += __longlong_as_double((long long)load_base(reinterpret_cast<const uint64_t *>(P.partial + (uint64_t)worker * P.partials + i)));
     }
     if (is_adam(K)) lr = ld_global(P.adam.lr);
-    const Early<K> early = load_early<K>(P, p, base, lane, kNotHeld);
+    const Early<K> early = load_early<K, false>(P, p, base, lane);
     if (P.norms != nullptr) {
         k.c = Factor{__uint_as_float(q.x), __uint_as_float(q.y)};
         k.step_size = __uint_as_float(q.z);
@@ -657,27 +657,35 @@ list_product_kernel(const __grid_constant__ ParamsOf<K> P)
         if (is_adam(K) && stop != 0u) return;          // the norm is not finite
     }
     if (is_adam(K)) adam_constants(P.adam, k);
-    products<K>(P, p, base, early, worker, k, lr, lane, kNotHeld);
+    products<K, false>(P, p, base, early, worker, k, lr, lane);
 }
 
+// Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
+//   pieces          16          32          48          64          96
+//   gather       4.3 / 6.0   4.6 / 5.6   5.2 / 5.6   5.3 / 5.7   8.3 / 5.8
+//   Adam step    6.2 / 6.7   7.8 / 6.7  10.1 / 7.2  10.3 / 7.3  17.0 / 7.8
+__host__ __device__ constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 16u : 64u; }
+
 // Both in one launch, grid (8 CTAs, workers), a cluster per worker.  The CTAs' sums are written to all CTAs' shared memory;
-// each adds them in the same order and forms norm and factor itself.  A warp's last item is still in its shared memory.
+// each adds them in the same order and forms norm and factor itself.  A warp has one item at most (cluster_most_pieces), whose products come
+// from its shared memory.
 // A chain of latencies: 4 x 65,536 fp32 gathered in 5.0 us, of which an empty launch of clusters is 2.1.
 template <ClipKind K>
 __global__ void __launch_bounds__(kClusterThreads, 1)
 list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
 {
+    static_assert(cluster_most_pieces(K) * 2 <= kClusterCtas * kClusterWarps && kPiece / 2 * 4 <= kHeldBytes, "an item, half a piece at most, per warp");
     extern __shared__ __align__(16) unsigned char held_bytes[];
     __shared__ double red[kClusterWarps], sums[kClusterCtas];
     __shared__ NormResult s_result;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, worker = blockIdx.y;
     const uint32_t held = (uint32_t)__cvta_generic_to_shared(held_bytes) + warp * kHeldBytes;
-    const uint32_t stride = kClusterCtas * kClusterWarps, items = P.L.pieces_n << P.split_log2, first = blockIdx.x * kClusterWarps + warp;
-    uint32_t c = first;
-    Piece last{}, p{};
-    ItemBase last_base{};
+    const uint32_t item = blockIdx.x * kClusterWarps + warp;
+    const bool busy = item < P.L.pieces_n << P.split_log2;
+    Piece p{};
+    ItemBase item_base{};
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this CTA runs: the others may write to it
-    if (c < items) p = load_item(P.L, c, P.split_log2);     // written before any launch
+    if (busy) p = load_item(P.L, item, P.split_log2);       // written before any launch
     depend_on_previous();
     const uint64_t *base = P.L.base + (uint64_t)worker * P.L.count;
     AdamStep k{};
@@ -692,15 +700,12 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
     if (is_adam(K) && threadIdx.x == kClusterThreads - 32) s_result.step_size = adam_step_size(P.adam, lr, t);
     if (is_adam(K) && threadIdx.x == kClusterThreads - 64) s_result.inv_sqrt_by2 = adam_inv_sqrt(P.adam, t);
     double s = 0.0;
-#pragma unroll 1
-    for (; c < items; c += stride) {
-        last = p;
-        if (c + stride < items) p = load_item(P.L, c + stride, P.split_log2);
-        else if (K != kNorm) last_base = load_item_base<K>(P, last, worker);
-        s += squares<K != kNorm>(last, base, P.src_flat, lane, K == kNorm || c + stride < items ? kNotHeld : held);
-    }
     Early<K> early{};
-    if (K != kNorm && first < items) early = load_early<K>(P, last, last_base, lane, held);
+    if (busy) {
+        if constexpr (K != kNorm) item_base = load_item_base<K>(P, p, worker);
+        s = squares<K != kNorm>(p, base, P.src_flat, lane, held);
+        if constexpr (K != kNorm) early = load_early<K, true>(P, p, item_base, lane, held);
+    }
     const double sum = sum_of_cta(s, red);
     __syncwarp();
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");             // all CTAs run
@@ -734,15 +739,7 @@ list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
             k.inv_sqrt_by2 = s_result.inv_sqrt_by2;
         }
         k.c = s_result.c;
-        if (first >= items) return;
-        products<K>(P, last, last_base, early, worker, k, lr, lane, held);
-#pragma unroll 1
-        for (c = first + (items - 1u - first) / stride * stride; c >= stride;) {
-            c -= stride;
-            p = load_item(P.L, c, P.split_log2);
-            last_base = load_item_base<K>(P, p, worker);
-            products<K>(P, p, last_base, load_early<K>(P, p, last_base, lane, kNotHeld), worker, k, lr, lane, kNotHeld);
-        }
+        if (busy) products<K, true>(P, p, item_base, early, worker, k, lr, lane, held);
     }
 }
 
@@ -1109,12 +1106,6 @@ static int launch_norm(ListParams &P, const thc_tensors *h, bool alone, cudaStre
     THC_CUDA(launch_after(list_norm_kernel<ADAM>, grid, kListThreads, 0, st, static_cast<const ListParams &>(P)));
     return THC_OK;
 }
-
-// Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
-//   pieces          16          32          48          64          96
-//   gather       4.3 / 6.0   4.6 / 5.6   5.2 / 5.6   5.3 / 5.7   8.3 / 5.8
-//   Adam step    6.2 / 6.7   7.8 / 6.7  10.1 / 7.2  10.3 / 7.3  17.0 / 7.8
-static constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 16u : 64u; }
 
 template <ClipKind K>
 static int launch_cluster(ParamsOf<K> &P, const thc_tensors *h, cudaStream_t st)
