@@ -14,7 +14,7 @@
  * worker's indices on one GPU).
  * A program's gradients and weights are many tensors: thc_tensors_create makes a list of them,
  * thc_grad_norm, thc_clip_grads and thc_gather_grads lead from it into a round, thc_scatter_grads
- * and thc_adamw from a round's output back to it.
+ * and thc_adamw from a round's output back to it; thc_void_round takes a round back whose gradients were not finite.
  *
  * Conventions shared by every call
  *   - "device" pointers are CUDA device addresses on the device that was current when the
@@ -373,7 +373,8 @@ int thc_scatter_grads(thc_ctx *ctx, const float *flat, double max_norm, const th
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,   t = step + 1,
  *     w = w (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
  * If the norm is not finite (in fp64, see thc_grad_norm) nothing is updated, step included, and THC_STATUS_NONFINITE is set.  Learning
- * rate and step count are read on the device, so that a captured step can be replayed.
+ * rate and step count are read on the device, so that a captured step can be replayed.  (The norm is the average's: that a gradient
+ * in front of the round was not finite shows in it by thc_void_round alone.)
  *   grad    device, sizes.d fp32, read
  *   list    n = 1: the model's weights, written
  *   lr      device, one fp32;   step  device, one int64 (steps done so far, >= 0), t is written back

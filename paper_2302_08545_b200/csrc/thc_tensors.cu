@@ -165,7 +165,7 @@ __device__ __forceinline__ Raw<T> held_unit(uint32_t held, uint32_t b, uint32_t 
 // ---------------------------------------------------------------------------------- norm
 // s + the squares of a unit.  fp32: each square in fp64, which no value leaves.  16 bits: the squares are exact in fp32, eight
 // of them are added there in three levels (3 x 2^-24 off at most, as all are positive) and the sum in fp64: a conversion and an fp64
-// operation per unit instead of eight, which were what bounded it (355M bf16: 125 us, now 106).  fp16's squares and their sums
+// operation per unit instead of eight, which were what bounded it (355M bf16 again and again: 125 us, now 106).  fp16's squares and their sums
 // stay within fp32; for bf16 a sum outside [2^-100, 2^126] (a square may have left fp32's range) is formed as for fp32, in a loop
 // (unrolled it takes the registers of the ordinary case: 111 us).
 template <uint32_t T>
@@ -661,15 +661,16 @@ list_product_kernel(const __grid_constant__ ParamsOf<K> P)
 }
 
 // Lists of at most this many pieces a worker take the cluster: as long as it is faster.  us, cluster / two launches:
-//   pieces          16          32          48          64          96
-//   gather       4.3 / 6.0   4.6 / 5.6   5.2 / 5.6   5.3 / 5.7   8.3 / 5.8
-//   Adam step    6.2 / 6.7   7.8 / 6.7  10.1 / 7.2  10.3 / 7.3  17.0 / 7.8
+// (captured launches in a row; beyond 64 a warp would have a second item)
+//   pieces            16          32          48          64
+//   gather        3.7 / 4.3   4.0 / 4.3   4.6 / 4.7   4.6 / 4.7
+//   Adam step     5.8 / 6.4   7.3 / 6.2  10.0 / 6.7  10.1 / 6.8
 __host__ __device__ constexpr uint32_t cluster_most_pieces(ClipKind k) { return is_adam(k) ? 16u : 64u; }
 
 // Both in one launch, grid (8 CTAs, workers), a cluster per worker.  The CTAs' sums are written to all CTAs' shared memory;
 // each adds them in the same order and forms norm and factor itself.  A warp has one item at most (cluster_most_pieces), whose products come
 // from its shared memory.
-// A chain of latencies: 4 x 65,536 fp32 gathered in 5.0 us, of which an empty launch of clusters is 2.1.
+// A chain of latencies: 4 x 65,536 fp32 gathered in 4.9 us, of which an empty launch of clusters is 2.1.
 template <ClipKind K>
 __global__ void __launch_bounds__(kClusterThreads, 1)
 list_cluster_kernel(const __grid_constant__ ParamsOf<K> P)
@@ -754,8 +755,10 @@ struct VoidParams {
     const float *ef[THC_MAX_WORKERS];
 };
 
-// Writes what a void round leaves (see thc.h), or, as nearly always, reads n numbers and ends.  d is a multiple of 64, every vector aligned
-// to 16 bytes.
+// Writes what a void round leaves (see thc.h), or, as nearly always, reads n numbers and ends: 1.0 to 1.1 us of a round of 28 us
+// (4 x 65,536 elements), of one of 38 us with residuals.  A launch of its own, so that the transform kernels do not change; a void round of
+// 8 x 25.6M with residuals takes 456 us here, 4 bytes written per element of the average and 8 moved per element of a residual.
+// d is a multiple of 64, every vector aligned to 16 bytes.
 __global__ void __launch_bounds__(kListThreads)
 void_round_kernel(const __grid_constant__ VoidParams P)
 {

@@ -177,7 +177,8 @@ class DataParallelRound:
     def step(self, grad, rnd: int):
         """Returns (out, scales, packed, total): the decompressed average and the intermediates
         (for checks; buffers of this object and of `ops`, overwritten by the next step).
-        Collectives are issued on the current stream of the tensors' device."""
+        Collectives are issued on the current stream of the tensors' device.
+        Gradients are finite, which is not looked at here (see step_tensors)."""
         ops, world, rank = self.ops, self.world, self.rank
         # 1. scales: max over workers of the per-worker M
         scales = ops.local_scales(grad)
