@@ -353,13 +353,16 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
  * ranks their sum over all ranks) is NaN or infinite,
  *     out[j] = NaN,   scales = 0,   grads[i] = ef[i],
  * and THC_STATUS_NONFINITE is set: thc_error_feedback then leaves each residual as it was, thc_adamw takes no step and
- * thc_scatter_grads hands the NaN on.  Otherwise nothing is written.  A norm that fp32 does not hold (it reads infinity) counts as infinite.
+ * thc_scatter_grads hands the NaN on.  Otherwise nothing is written.  A norm that fp32 does not hold (it reads infinity) counts as infinite,
+ * and so does, where max_norm does not keep what is sent below it, one above 2^126 / (sqrt(B) max(1, t_p)) (2 x 10^34 for B = 2^22 and
+ * the paper's t_p): the transform's fp32 sums could leave fp32's range, and the residual with them.
  *   list        the gradients that were gathered
+ *   max_norm    what they were gathered with, >= 0
  *   norms       device, n fp32, read
  *   scales      device, thc_sizes_t.scales_count fp32 of the list's d;   out  device, sizes.d fp32
  *   grads, ef   host arrays of n device pointers as in thc_error_feedback, all apart from each other (THC_EINVAL); both
  *               NULL without residuals (fp32 contexts only, THC_EUNSUPPORTED otherwise)                     */
-int thc_void_round(thc_ctx *ctx, const thc_tensors *list, const float *norms, float *scales, float *out,
+int thc_void_round(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *norms, float *scales, float *out,
                    float *const *grads_or_null, const float *const *ef_or_null, void *stream);
 
 /* The way out of a round: the flat average that thc_decompress wrote, clipped by the norm of what belongs to

@@ -479,7 +479,7 @@ static PyObject *b_gather_grads(ARGS)
     CALL(thc_gather_grads(ctx, list, most, (const float *const *)array_of(&e), array_of(&f), norms, ws, wb, st));
 }
 
-/* (handle, list, norms, scales, out, grads, ef, stream) */
+/* (handle, list, max_norm, norms, scales, out, grads, ef, stream) */
 static PyObject *b_void_round(ARGS)
 {
     void *ctx_p, *st, *norms, *scales, *out;
@@ -487,14 +487,15 @@ static PyObject *b_void_round(ARGS)
     thc_tensors_sizes_t sz;
     thc_sizes_t round;
     list_t g, e;
+    double most;
     int rc;
     (void)self;
-    if (want(na, 8) || address(a[0], &ctx_p) || list_of(a[1], &list, &sz) || list_stream(a[7], &sz, &st)) return NULL;
+    if (want(na, 9) || address(a[0], &ctx_p) || list_of(a[1], &list, &sz) || list_stream(a[8], &sz, &st) || real(a[2], &most)) return NULL;
     memset(&round, 0, sizeof round);
     if (ctx_p != NULL && sz.n != 0) thc_sizes(ctx_p, sz.d, 1, &round);
-    if (vector(a[2], &norms, F32, sz.n, &sz, "norms") || vector(a[3], &scales, F32, round.scales_count, &sz, "scales") ||
-        vector(a[4], &out, F32, sz.d, &sz, "out") || vectors(a[5], &g, F32, &sz, "grads") || vectors(a[6], &e, F32, &sz, "ef")) return NULL;
-    CALL(thc_void_round(ctx_p, list, norms, scales, out, (rot_t)array_of(&g), (const float *const *)array_of(&e), st));
+    if (vector(a[3], &norms, F32, sz.n, &sz, "norms") || vector(a[4], &scales, F32, round.scales_count, &sz, "scales") ||
+        vector(a[5], &out, F32, sz.d, &sz, "out") || vectors(a[6], &g, F32, &sz, "grads") || vectors(a[7], &e, F32, &sz, "ef")) return NULL;
+    CALL(thc_void_round(ctx_p, list, most, norms, scales, out, (rot_t)array_of(&g), (const float *const *)array_of(&e), st));
 }
 
 /* (handle, flat, max_norm, list, norms, workspace, stream) */

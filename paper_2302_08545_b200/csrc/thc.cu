@@ -721,7 +721,7 @@ int thc::cuda_fail(cudaError_t e)
     return THC_ECUDA;
 }
 
-CtxView thc::view_of(const thc_ctx *ctx) { return CtxView{ctx->dev, ctx->device, ctx->sm_count, ctx->cfg.in_dtype}; }
+CtxView thc::view_of(const thc_ctx *ctx) { return CtxView{ctx->dev, ctx->device, ctx->sm_count, ctx->cfg.in_dtype, ctx->cfg.log2_block, ctx->cfg.t_p}; }
 
 // No launch takes more dynamic shared memory: a pipeline CTA, a tile of 2^14 or one of 2^13 with the constants
 // of 1024 blocks, each with a table of 256 entries, take up to 101 KB.  (More than half an SM's 228 KB, so that

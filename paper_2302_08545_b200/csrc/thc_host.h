@@ -22,6 +22,8 @@ struct CtxView {
     int device;                 // -1: no CUDA device, host-only context
     int sm_count;
     uint32_t in_dtype;
+    uint32_t log2_block;
+    double t_p;
 };
 CtxView view_of(const thc_ctx *ctx);
 

@@ -750,6 +750,7 @@ struct VoidParams {
     float *scales, *out;
     uint64_t d, scales_n;
     uint32_t n, residuals;       // residuals: n or 0
+    float most;                  // a larger norm, or a NaN, makes the round void
     DeviceBlock *dev;
     float *grads[THC_MAX_WORKERS];
     const float *ef[THC_MAX_WORKERS];
@@ -763,7 +764,7 @@ __global__ void __launch_bounds__(kListThreads)
 void_round_kernel(const __grid_constant__ VoidParams P)
 {
     depend_on_previous();
-    const bool bad = threadIdx.x < P.n && !isfinite(ld_global(P.norms + threadIdx.x));
+    const bool bad = threadIdx.x < P.n && !(ld_global(P.norms + threadIdx.x) <= P.most);
     if (!__syncthreads_or(bad)) return;
     const uint64_t first = (uint64_t)blockIdx.x * kListThreads + threadIdx.x, stride = (uint64_t)gridDim.x * kListThreads;
     const float nan = __uint_as_float(0x7FFFFFFFu);
@@ -1239,12 +1240,19 @@ int thc_gather_grads(thc_ctx *ctx, const thc_tensors *list, double max_norm, con
     return launch_call<kGatherF32>(P, ctx, list, max_norm, norms, workspace, stream);
 }
 
-int thc_void_round(thc_ctx *ctx, const thc_tensors *list, const float *norms, float *scales, float *out, float *const *grads_or_null,
-                   const float *const *ef_or_null, void *stream)
+// Norms up to here pass a block of the context.  A rotation adds up to sqrt(B) |x| before it is scaled, the one back B times M = t_p |x| / sqrt(B): with
+// 2^126 for either the fourfold is left for residuals and roundings.
+static double transform_limit(const CtxView &view)
+{
+    return 0x1p126 / (sqrt((double)(1ull << view.log2_block)) * std::max(1.0, view.t_p));
+}
+
+int thc_void_round(thc_ctx *ctx, const thc_tensors *list, double max_norm, const float *norms, float *scales, float *out,
+                   float *const *grads_or_null, const float *const *ef_or_null, void *stream)
 {
     int rc = check_list(ctx, list);
     if (rc != THC_OK) return rc;
-    if (norms == nullptr || !aligned4(norms) || scales == nullptr || !aligned16(scales) || out == nullptr || !aligned16(out)) return THC_EINVAL;
+    if (!(max_norm >= 0.0) || norms == nullptr || !aligned4(norms) || scales == nullptr || !aligned16(scales) || out == nullptr || !aligned16(out)) return THC_EINVAL;
     if ((grads_or_null == nullptr) != (ef_or_null == nullptr)) return THC_EINVAL;
     if (ef_or_null != nullptr && view_of(ctx).in_dtype != THC_F32) return THC_EUNSUPPORTED;
     thc_sizes_t sz;
@@ -1257,7 +1265,9 @@ int thc_void_round(thc_ctx *ctx, const thc_tensors *list, const float *norms, fl
     P.d = list->d;
     P.scales_n = sz.scales_count;
     P.n = list->n;
-    P.dev = view_of(ctx).dev;
+    const CtxView view = view_of(ctx);
+    P.dev = view.dev;
+    P.most = max_norm <= transform_limit(view) ? 0x1.fffffep127f : (float)transform_limit(view);   // (clipped: any finite norm)
     struct Span { uint64_t lo, bytes; };
     Span written[THC_MAX_WORKERS + 2], read[THC_MAX_WORKERS + 1];
     uint32_t writes = 0, reads = 0;

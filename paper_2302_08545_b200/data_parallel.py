@@ -122,9 +122,9 @@ class CudaOps:
     def residual(self, grad, packed, rnd: int, scales, ef):
         self.ctx.error_feedback([grad], [packed], self.d, rnd, scales, [ef], self.workspace)
 
-    def void(self, tensors, norms, grad, scales, out, ef=None):
+    def void(self, tensors, max_norm, norms, grad, scales, out, ef=None):
         """After a round: nothing if `norms` (the sum of all ranks') is finite, else see thc.Context.void_round."""
-        self.ctx.void_round(tensors, norms, scales, out, None if ef is None else [grad], None if ef is None else [ef])
+        self.ctx.void_round(tensors, max_norm, norms, scales, out, None if ef is None else [grad], None if ef is None else [ef])
 
     def scatter(self, out, tensors, max_norm: float = math.inf):
         """The average, clipped by its norm, to tensors."""
@@ -229,7 +229,7 @@ class DataParallelRound:
             dist.all_reduce(self._norms, group=self.group)
         out, scales, packed, total = self.step(grad, rnd)
         if norm is not None:
-            self.ops.void(tensors, self._norms, grad, scales, out, ef)
+            self.ops.void(tensors, max_norm, self._norms, grad, scales, out, ef)
         if ef is not None:
             self.ops.residual(grad, packed, rnd, scales, ef)
         return out, scales, packed, total

@@ -106,7 +106,7 @@ class TensorRound:
     that are allocated anew every step (torch's zero_grad sets them to None) are given to it by assign.  With error feedback each worker's
     residual of one round is added to its gradients of the next (fp32 contexts).
 
-    A round in which a worker's norm is not finite is void: its average is NaN in every element, so that adamw takes no step and
+    A round in which a worker's norm is not finite (see thc_void_round for how large it may be) is void: its average is NaN in every element, so that adamw takes no step and
     scatter hands the NaN on, and every worker keeps its residual; the next round is as if it had not been."""
 
     def __init__(self, ctx: thc.Context, grads, error_feedback: bool = False):
@@ -132,7 +132,7 @@ class TensorRound:
         r = self.round
         self.ctx.gather_grads(self.grads, max_norm, r.grads, self.norms, self.workspace, ef=self.ef, stream=stream)
         r.run(rnd, fused=True, stream=stream)
-        self.ctx.void_round(self.grads, self.norms, r.scales, r.out, None if self.ef is None else r.grads, self.ef, stream)
+        self.ctx.void_round(self.grads, max_norm, self.norms, r.scales, r.out, None if self.ef is None else r.grads, self.ef, stream)
         if self.ef is not None:
             self.ctx.error_feedback(r.grads, r.packed, r.d, rnd, r.scales, self.ef, r.workspace, stream)
         return r.out

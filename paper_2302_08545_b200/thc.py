@@ -111,7 +111,7 @@ def lib():
     L.thc_grad_norm.argtypes = [vp, vp, vp, vp, u64, vp]
     L.thc_clip_grads.argtypes = [vp, vp, f64, vp, vp, vp, u64, vp]
     L.thc_gather_grads.argtypes = [vp, vp, f64, pp, pp, vp, vp, u64, vp]
-    L.thc_void_round.argtypes = [vp, vp, vp, vp, vp, pp, pp, vp]
+    L.thc_void_round.argtypes = [vp, vp, f64, vp, vp, vp, pp, pp, vp]
     L.thc_scatter_grads.argtypes = [vp, vp, f64, vp, vp, vp, u64, vp]
     L.thc_adamw.argtypes = [vp, ctypes.POINTER(_AdamwConfig), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
     L.thc_debug_skip_tasks.argtypes = [vp, u32]
@@ -359,10 +359,11 @@ class Context:
         _check(self._call.gather_grads(self._handle, tensors._handle, max_norm, ef, flats, norms, workspace,
                                        self.in_dtype == THC_BF16, stream), "thc_gather_grads")
 
-    def void_round(self, tensors: Tensors, norms, scales, out, grads=None, ef=None, stream=None):
-        """Behind the call that writes the average `out`, before `error_feedback`: if a worker's norm is not finite, the average
-        becomes NaN, the scales 0 and each of `grads` its residual `ef`, so that no residual changes and no step is taken."""
-        _check(self._call.void_round(self._handle, tensors._handle, norms, scales, out, grads, ef, stream), "thc_void_round")
+    def void_round(self, tensors: Tensors, max_norm: float, norms, scales, out, grads=None, ef=None, stream=None):
+        """Behind the call that writes the average `out`, before `error_feedback`: if a worker's norm is not finite (or, not clipped by
+        `max_norm`, past what the transform holds), the average becomes NaN, the scales 0 and each of `grads` its residual
+        `ef`, so that no residual changes and no step is taken."""
+        _check(self._call.void_round(self._handle, tensors._handle, max_norm, norms, scales, out, grads, ef, stream), "thc_void_round")
 
     def scatter_grads(self, flat, max_norm: float, tensors: Tensors, norms, workspace, stream=None):
         """The flat average, clipped, to the tensors."""

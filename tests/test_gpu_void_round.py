@@ -38,13 +38,13 @@ def test_what_is_written(size, n, k, residuals):
     norms = torch.rand(n, device="cuda")
     every = [*room, scales, norms]
     old = [x.clone() for x in every]
-    ctx.void_round(lst, norms, scales[:scales_n], out, grads, ef)
+    ctx.void_round(lst, math.inf, norms, scales[:scales_n], out, grads, ef)
     assert all(torch.equal(x, y) for x, y in zip(every, old)) and ctx.status() == 0
     for i, value in {0: math.nan, n - 1: math.inf}.items():
         for x, y in zip(every, old):
             x.copy_(y)
         norms[i] = value
-        ctx.void_round(lst, norms, scales[:scales_n], out, grads, ef)
+        ctx.void_round(lst, math.inf, norms, scales[:scales_n], out, grads, ef)
         assert ctx.status() == thc.STATUS_NONFINITE
         assert bool(torch.isnan(out).all()) and not bool(scales[:scales_n].any())
         assert torch.equal(scales[scales_n:], old[-2][scales_n:])
@@ -167,3 +167,38 @@ def test_step_tensors_of_one_rank():
         assert torch.equal(dp.step_tensors(lst, 2, max_norm=3.0, ef=ef)[0], again) and not ctx.status() & thc.STATUS_NONFINITE
     finally:
         dist.destroy_process_group()
+
+
+@pytest.mark.parametrize("k", [10, 14, 16, 20])
+def test_finite_gradients_past_what_the_transform_holds(k):
+    """Not clipped, a norm above 2^126 / (sqrt(B) t_p) makes a round void and leaves the residuals finite; up to there, and clipped at any
+    norm, the round is served: values of one kind, of random signs, and a single one."""
+    from paper_2302_08545_b200 import runner, thc, workloads as W
+    ctx = context(n=2, k=k)
+    limit = 2.0 ** 126 / (2.0 ** (k / 2) * W.T_P["1/32"])
+    size = 3 * (1 << min(k, 16))
+    grads = T.make([size, 77], ["f32"], 2, seed=1)
+    signs = torch.randn(size, device="cuda")
+    kinds = [torch.ones(size, device="cuda"), signs, torch.nn.functional.one_hot(torch.tensor(5), size).float().cuda()]
+    for kind in kinds:
+        tr = runner.TensorRound(ctx, grads, error_feedback=True)
+        unit = (kind.double() / torch.linalg.vector_norm(kind.double())).float()
+        for x in (grads[0][1], grads[1][1]):
+            x.zero_()
+        rnd = 0
+        for norm, max_norm, void in ((0.99 * limit, math.inf, False), (1.01 * limit, math.inf, True), (1.01 * limit, 1.0, False), (2e38, math.inf, True),
+                                     (2e38, 1.0, False), (2e38, 2.0 * limit, True), (1.0, math.inf, False)):
+            grads[0][0].copy_(unit * norm)
+            grads[1][0].copy_(signs * 1e-3)
+            held = [x.clone() for x in tr.ef]
+            for e in tr.ef if not void else []:
+                e.zero_()                          # (a residual of a step at the limit would be added to the next one)
+            out = tr.run(rnd, max_norm=max_norm)
+            flags = ctx.status()
+            assert all(bool(torch.isfinite(e).all()) for e in tr.ef), (norm, max_norm)
+            if void:
+                assert bool(torch.isnan(out).all()) and flags & thc.STATUS_NONFINITE
+                assert all(torch.equal(x, y) for x, y in zip(tr.ef, held))
+            else:
+                assert bool(torch.isfinite(out).all()) and not flags & thc.STATUS_NONFINITE
+            rnd += 1

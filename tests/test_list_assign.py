@@ -50,7 +50,7 @@ assert assign(1) == thc.THC_ECUDA
 clipped = lst(numel, [0] * k, at=1 << 41, step=1 << 12)
 calls = [lambda: gather(1 << 50), lambda: call("thc_grad_norm", h, N), lambda: call("thc_clip_grads", h, 1.0, None, N),
          lambda: call("thc_clip_grads", clipped, 1.0, h, N), lambda: call("thc_scatter_grads", 1 << 50, 1.0, h, N),
-         lambda: L.thc_void_round(c._h, h, N, 1 << 51, 1 << 50, None, None, None)]
+         lambda: L.thc_void_round(c._h, h, 1.0, N, 1 << 51, 1 << 50, None, None, None)]
 log()
 assert [f() for f in calls] == [E] * len(calls) and log() == []
 assert assign(0) == thc.THC_ECUDA and gather(1 << 50) == E

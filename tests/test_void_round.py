@@ -28,7 +28,7 @@ class TensorOps(OracleOps):                        # tensors are concatenated, c
     def residual(self, grad, packed, rnd, scales, ef):
         z = O.unpack(np.array(packed.numpy()), (d + 255) // 256 * 256, 4)
         ef.copy_(torch.from_numpy(O.error_feedback(grad.numpy(), z, scales.numpy(), cfg, rnd)))
-    def void(self, tensors, norms, grad, scales, out, ef=None):      # the definition of thc_void_round
+    def void(self, tensors, max_norm, norms, grad, scales, out, ef=None):      # the definition of thc_void_round
         if not bool(torch.isfinite(norms).all()):
             out.fill_(float("nan"))
             scales.zero_()
@@ -85,10 +85,10 @@ E, U = thc.THC_EINVAL, thc.THC_EUNSUPPORTED
 h, h2 = lst([100, 70], [0, 0]), lst([100, 70], [1, 0], 2, at=1 << 40)
 F = [(1 << 46) + (i << 20) for i in range(8)]
 S = 1 << 47                             # one scale: 256 elements in blocks of 2^10
-def void(t=h, norms=N, scales=S, out=F[0], grads=None, ef=None, ctx=c):
-    return L.thc_void_round(ctx._h if ctx else None, t, norms, scales, out, grads, ef, None)
+def void(t=h, norms=N, scales=S, out=F[0], grads=None, ef=None, ctx=c, most=math.inf):
+    return L.thc_void_round(ctx._h if ctx else None, t, most, norms, scales, out, grads, ef, None)
 log()
-assert void(ctx=None) == E and void(t=None) == E
+assert void(ctx=None) == E and void(t=None) == E and void(most=-1.0) == E and void(most=math.nan) == E
 assert void(norms=None) == E and void(norms=N + 2) == E and void(scales=None) == E and void(scales=S + 4) == E
 assert void(out=None) == E and void(out=F[0] + 8) == E
 assert void(grads=p(F[1])) == E and void(ef=p(F[1])) == E                  # one without the other
@@ -116,12 +116,12 @@ def test_tensors_that_the_binding_refuses():
     c = thc.Context(bits=4, granularity=30, table=W.TABLES[(4, 30)], t_p=2.0, log2_block=6, seed=1)
     t = thc.Tensors(c, [[torch.zeros(100)], [torch.zeros(100)]])
     f, norms, scales = [torch.zeros(t.d) for _ in range(5)], torch.zeros(2), torch.zeros(2)
-    for call in (lambda: c.void_round(t, norms[:1], scales, f[0], stream=0), lambda: c.void_round(t, norms, scales[:1], f[0], stream=0),
-                 lambda: c.void_round(t, norms, scales, f[0][:-1], stream=0), lambda: c.void_round(t, norms, scales, f[0].half(), stream=0),
-                 lambda: c.void_round(t, norms, scales, f[0], grads=f[1:2], ef=f[3:5], stream=0),
-                 lambda: c.void_round(t, norms, scales, f[0], grads=f[1:3], ef=[f[3], f[4][1:]], stream=0)):
+    for call in (lambda: c.void_round(t, 1.0, norms[:1], scales, f[0], stream=0), lambda: c.void_round(t, 1.0, norms, scales[:1], f[0], stream=0),
+                 lambda: c.void_round(t, 1.0, norms, scales, f[0][:-1], stream=0), lambda: c.void_round(t, 1.0, norms, scales, f[0].half(), stream=0),
+                 lambda: c.void_round(t, 1.0, norms, scales, f[0], grads=f[1:2], ef=f[3:5], stream=0),
+                 lambda: c.void_round(t, 1.0, norms, scales, f[0], grads=f[1:3], ef=[f[3], f[4][1:]], stream=0)):
         with pytest.raises(ValueError):
             call()
     with pytest.raises(thc.ThcError) as e:
-        c.void_round(t, norms, scales, f[0], grads=f[1:3], ef=f[3:5], stream=0)
+        c.void_round(t, 1.0, norms, scales, f[0], grads=f[1:3], ef=f[3:5], stream=0)
     assert e.value.code == thc.THC_ECUDA
